@@ -60,7 +60,8 @@ typedef enum {
   VP_ERR_WORKSPACE = 6,   /* workspace pointer NULL or smaller than the size the library asked for */
   VP_ERR_TARGET = 7,      /* (vp_ce_check) some target was outside [0, V) and not ignore_index */
   VP_ERR_HIP = 8,         /* a HIP runtime call or a kernel launch failed */
-  VP_ERR_UNSUPPORTED = 9  /* valid request the library does not implement */
+  VP_ERR_UNSUPPORTED = 9, /* valid request the library does not implement */
+  VP_ERR_VALUE = 10       /* a parameter (eps, beta, a clip bound, ...) is outside its range */
 } vp_status;
 
 typedef enum {
@@ -213,6 +214,146 @@ vp_status vp_ce_plan_info(const vp_problem* prob, vp_plan_info* info);
  * this workspace found (synchronises `stream`).  Returns VP_ERR_TARGET if it is
  * non-zero.  *bad_targets may be NULL. */
 vp_status vp_ce_check(const void* ws, void* stream, int64_t* bad_targets);
+
+/* ------------------------------------------------------------------------------
+ * Layer norm of the hidden states, in front of the projection (H of vp_ce_forward is
+ * its Y; its dY is the dH of vp_ce_backward):
+ *   mu_t  = (1/d) sum_j x_tj                        (0 with VP_NORM_RMS)
+ *   r_t   = ((1/d) sum_j (x_tj - mu_t)^2 + eps)^(-1/2)
+ *   y_tj  = gamma_j (x_tj - mu_t) r_t + beta_j
+ * Sums are float32; y is rounded once, to nearest even. */
+#define VP_NORM_RMS 2u /* no mean: mu_t = 0 in the forward and the backward */
+
+typedef struct {
+  int64_t T;      /* tokens, 0..2^23 - 256 (T == 0: nothing to do in the forward) */
+  int64_t d;      /* width, 8..32768 and a multiple of 8 (VP_ERR_SHAPE otherwise) */
+  int32_t dtype;  /* vp_dtype of X, gamma, beta and Y */
+  uint32_t flags; /* VP_NORM_RMS, VP_ACCUMULATE_DW */
+  double eps;     /* >= 0 and finite (VP_ERR_VALUE otherwise) */
+} vp_norm;
+
+/* Workspace of vp_norm_backward in bytes.  Host only. */
+vp_status vp_norm_workspace_size(const vp_norm* norm, size_t* bwd_bytes);
+
+/* X: device [T, d] of dtype; gamma, beta: device [d] of dtype, beta may be NULL (no
+ * bias); Y: device [T, d] of dtype, no part of X; mean, rstd: device float32 [T], what
+ * the backward replays from (mean is neither written nor read with VP_NORM_RMS and may
+ * then be NULL).  X, gamma, beta and Y must be 16-byte aligned. */
+vp_status vp_norm_forward(const vp_norm* norm, const void* X, const void* gamma, const void* beta,
+                          void* Y, float* mean, float* rstd, void* stream);
+
+/* With xh_tj = (x_tj - mu_t) r_t and g_tj = dy_tj gamma_j:
+ *   dx_tj    = r_t (g_tj - (1/d) sum_k g_tk - xh_tj (1/d) sum_k g_tk xh_tk)
+ *              (without the first sum with VP_NORM_RMS)
+ *   dgamma_j = sum_t dy_tj xh_tj,   dbeta_j = sum_t dy_tj
+ * dY: device float32 [T, d]; dX: device float32 [T, d], overwritten; it may be dY
+ * itself.  dgamma, dbeta: device float32 [d], overwritten, or added to with
+ * VP_ACCUMULATE_DW; dbeta may be NULL (not computed).  All but mean and rstd must be
+ * 16-byte aligned, and so must ws.  T == 0 gives dgamma = dbeta = 0 (or leaves them
+ * when accumulating).  Two calls on the same inputs give the same bits. */
+vp_status vp_norm_backward(const vp_norm* norm, const void* X, const void* gamma, const float* mean,
+                           const float* rstd, const float* dY, float* dX, float* dgamma,
+                           float* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------
+ * Losses of whole sequences, behind the projection.  They read the per-token loss of
+ * vp_ce_forward (loss_t = -log p of the target) and write the per-token gradient that
+ * vp_ce_backward takes as grad_loss.
+ *
+ * The T tokens hold S sequences one after the other: sequence s is the tokens
+ * start[s] .. start[s + 1] - 1 (start: device int32 [S + 1], never decreasing, within
+ * 0..T; a sequence may be empty; tokens before start[0] or from start[S] on belong to
+ * none).  A token counts if it belongs to a sequence and targets[t] != ignore_index:
+ * what any other token's entry of a per-token array holds is not used (it may be NaN),
+ * and its gradient is 0.  With n_s the counting tokens of sequence s, a sum over it is
+ * weighted by c_s = 1, or with VP_SEQ_MEAN by c_s = 1 / n_s (0 where n_s == 0).
+ * Sums are float64, results are rounded once to float32.
+ *
+ * Every offset is held against 0..T before it is used as one: wrong offsets never lead
+ * outside an array.  A sequence whose own two offsets decrease or leave 0..T gets NaN
+ * results; what the other sequences of such a call get is not specified. */
+#define VP_SEQ_MEAN 4u
+
+typedef struct {
+  int64_t T;            /* tokens, 0..2^23 - 256 */
+  int64_t S;            /* sequences, 0..2^22 */
+  int64_t ignore_index; /* target value of a token that does not count */
+  uint32_t flags;       /* VP_SEQ_MEAN */
+} vp_sequences;
+
+/* Workspace of vp_pref_forward and of vp_policy_forward in bytes.  Host only. */
+vp_status vp_seq_workspace_size(const vp_sequences* seq, size_t* bytes);
+
+typedef enum {
+  VP_PREF_LOGISTIC = 0,
+  VP_PREF_SQUARED = 1
+} vp_pref_kind;
+
+/* Preference loss over pairs: pair i is sequence 2i (preferred) and 2i + 1 (rejected),
+ * so S must be even (VP_ERR_SHAPE otherwise).  With R_s = c_s sum_t (ref_t - loss_t),
+ * the log ratio of the policy to the reference:
+ *   reward_s = beta R_s,   z_i = reward_2i - reward_{2i+1} - margin
+ *   VP_PREF_LOGISTIC: pair_loss_i = (1 - smoothing) log(1 + e^-z) + smoothing log(1 + e^z)
+ *   VP_PREF_SQUARED:  pair_loss_i = ((z - 1/2) / beta)^2 */
+typedef struct {
+  int32_t kind;     /* vp_pref_kind (VP_ERR_VALUE otherwise, as for the rest) */
+  double beta;      /* > 0 and finite */
+  double margin;    /* finite */
+  double smoothing; /* 0..1/2, 0 for VP_PREF_SQUARED */
+} vp_preference;
+
+/* targets: device int64 [T]; loss, ref_loss: device float32 [T], ref_loss may be NULL
+ * (ref_t = 0); pair_loss: device float32 [S/2]; reward: device float32 [S];
+ * coef: device float32 [S], what the backward replays from: d pair_loss / d loss_t for
+ * the counting tokens of each sequence.  ws: 16-byte aligned. */
+vp_status vp_pref_forward(const vp_sequences* seq, const vp_preference* pref, const int32_t* start,
+                          const int64_t* targets, const float* loss, const float* ref_loss,
+                          float* pair_loss, float* reward, float* coef, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/* grad_loss[t] = grad_pair[s/2] coef[s] for the counting tokens of sequence s, else 0;
+ * device float32 [T], every entry written.  grad_pair: device float32 [S/2], the
+ * upstream gradient of each pair's loss.  start and targets as in the forward. */
+vp_status vp_pref_backward(const vp_sequences* seq, const int32_t* start, const int64_t* targets,
+                           const float* coef, const float* grad_pair, float* grad_loss,
+                           void* stream);
+
+/* Clipped policy loss with a KL term.  With A the advantage, rho_t = e^(old_t - loss_t)
+ * and q_t = loss_t - ref_t:
+ *   kl_t = e^q - q - 1          (estimates KL(policy || reference); >= 0)
+ *   l_t  = -min(rho_t A, clip(rho_t, 1 - clip_low, 1 + clip_high) A) + kl_coef kl_t
+ *   seq_loss_s = c_s sum_t l_t,   seq_kl_s = c_s sum_t kl_t
+ * A token is clipped where the minimum is the clipped term alone (A > 0 and rho_t >
+ * 1 + clip_high, or A < 0 and rho_t < 1 - clip_low; decided in float64): there the
+ * first term has no gradient. */
+#define VP_ADV_PER_TOKEN 8u
+
+typedef struct {
+  double clip_low;  /* 0..1 (VP_ERR_VALUE otherwise, as for the rest) */
+  double clip_high; /* >= 0, may be infinite */
+  double kl_coef;   /* >= 0 and finite */
+  uint32_t flags;   /* VP_ADV_PER_TOKEN */
+} vp_policy;
+
+/* loss, old_loss, ref_loss: device float32 [T]; old_loss may be NULL (the policy that
+ * drew the tokens is this one: rho = 1 with the gradient of rho), ref_loss may be NULL
+ * (kl_t = 0); advantage: device float32 [S], or [T] with VP_ADV_PER_TOKEN; seq_loss,
+ * seq_kl: device float32 [S]; clipped, tokens: device int32 [S], the clipped and the
+ * counting tokens.  ws: 16-byte aligned. */
+vp_status vp_policy_forward(const vp_sequences* seq, const vp_policy* policy, const int32_t* start,
+                            const int64_t* targets, const float* loss, const float* old_loss,
+                            const float* ref_loss, const float* advantage, float* seq_loss,
+                            float* seq_kl, int32_t* clipped, int32_t* tokens, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/* grad_loss[t] = grad_seq[s] c_s (A rho_t [not clipped] + kl_coef (e^q - 1)) for the
+ * counting tokens of sequence s, else 0; device float32 [T], every entry written.
+ * grad_seq: device float32 [S], the upstream gradient of each seq_loss; tokens: from
+ * the forward (read with VP_SEQ_MEAN alone); the rest as in the forward. */
+vp_status vp_policy_backward(const vp_sequences* seq, const vp_policy* policy, const int32_t* start,
+                             const int64_t* targets, const float* loss, const float* old_loss,
+                             const float* ref_loss, const float* advantage, const int32_t* tokens,
+                             const float* grad_seq, float* grad_loss, void* stream);
 
 const char* vp_status_str(vp_status s);
 int vp_abi_version(void);

@@ -9,6 +9,12 @@ The low-level functions carry the C names (``vp_ce_workspace_size``,
 ``vp_ce_forward``, ``vp_ce_backward``, ``vp_ce_check``, ``vp_status_str``,
 ``vp_abi_version``) and take torch tensors; ``forward`` and ``backward``
 allocate outputs and workspace and call them.
+
+``head`` binds the operators around the projection in the same way: a layer norm in
+front of it (``vp_norm_*``, ``layer_norm``; ``forward`` and ``backward`` take one as
+``norm=``), and behind it a preference loss (``vp_pref_*``, ``preference_forward`` /
+``_backward``) and a clipped policy loss (``vp_policy_*``, ``policy_forward`` /
+``_backward``) of whole sequences, between the per-token loss and its gradient.
 """
 from __future__ import annotations
 
@@ -21,13 +27,18 @@ LIB_PATH = os.path.join(_PKG, "libvpce.so")
 
 VP_OK, VP_ERR_NULL, VP_ERR_SHAPE, VP_ERR_DTYPE, VP_ERR_ORDER = 0, 1, 2, 3, 4
 VP_ERR_ALIGN, VP_ERR_WORKSPACE, VP_ERR_TARGET, VP_ERR_HIP, VP_ERR_UNSUPPORTED = 5, 6, 7, 8, 9
+VP_ERR_VALUE = 10
 VP_F32, VP_BF16 = 0, 1
-VP_ACCUMULATE_DW = 1
+VP_ACCUMULATE_DW, VP_NORM_RMS, VP_SEQ_MEAN, VP_ADV_PER_TOKEN = 1, 2, 4, 8
+VP_PREF_LOGISTIC, VP_PREF_SQUARED = 0, 1
 VP_MAX_SHARDS = 64
 
 EXPORTED = ("vp_ce_workspace_size", "vp_ce_forward", "vp_ce_forward_noalloc", "vp_ce_backward",
             "vp_ce_state_init",
             "vp_ce_fold_shard", "vp_ce_fold_finalize", "vp_ce_plan_info", "vp_ce_check",
+            "vp_norm_workspace_size", "vp_norm_forward", "vp_norm_backward",
+            "vp_seq_workspace_size", "vp_pref_forward", "vp_pref_backward",
+            "vp_policy_forward", "vp_policy_backward",
             "vp_status_str", "vp_abi_version")
 
 
@@ -54,6 +65,26 @@ class vp_problem(ctypes.Structure):
         ("flags", ctypes.c_uint32),
         ("strip_elems", ctypes.c_int64),
     ]
+
+
+class vp_norm(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("d", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("eps", ctypes.c_double)]
+
+
+class vp_sequences(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("S", ctypes.c_int64), ("ignore_index", ctypes.c_int64),
+                ("flags", ctypes.c_uint32)]
+
+
+class vp_preference(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("beta", ctypes.c_double), ("margin", ctypes.c_double),
+                ("smoothing", ctypes.c_double)]
+
+
+class vp_policy(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_coef", ctypes.c_double),
+                ("flags", ctypes.c_uint32)]
 
 
 _lib = None
@@ -95,6 +126,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vp_ce_plan_info.argtypes = [vp, P(vp_plan_info)]
     lib.vp_ce_check.restype = ctypes.c_int
     lib.vp_ce_check.argtypes = [vptr, vptr, P(ctypes.c_int64)]
+    size = ctypes.c_size_t
+    for fn, args in ((lib.vp_norm_workspace_size, [P(vp_norm), P(size)]),
+                     (lib.vp_norm_forward, [P(vp_norm)] + [vptr] * 7),
+                     (lib.vp_norm_backward, [P(vp_norm)] + [vptr] * 9 + [size, vptr]),
+                     (lib.vp_seq_workspace_size, [P(vp_sequences), P(size)]),
+                     (lib.vp_pref_forward, [P(vp_sequences), P(vp_preference)] + [vptr] * 8 + [size, vptr]),
+                     (lib.vp_pref_backward, [P(vp_sequences)] + [vptr] * 6),
+                     (lib.vp_policy_forward, [P(vp_sequences), P(vp_policy)] + [vptr] * 11 + [size, vptr]),
+                     (lib.vp_policy_backward, [P(vp_sequences), P(vp_policy)] + [vptr] * 10)):
+        fn.restype = ctypes.c_int
+        fn.argtypes = args
     _lib = lib
     return lib
 
@@ -413,6 +455,13 @@ def _dtype_code(t) -> int:
     raise TypeError(f"unsupported dtype {t.dtype} (bfloat16 or float32)")
 
 
+from .head import (HeadNorm, Norm, Policy, Preference, Sequences, layer_norm,  # noqa: E402
+                   layer_norm_backward, policy_backward, policy_forward, preference_backward,
+                   preference_forward, vp_norm_backward, vp_norm_forward, vp_norm_workspace_size,
+                   vp_policy_backward, vp_policy_forward, vp_pref_backward, vp_pref_forward,
+                   vp_seq_workspace_size)
+
+
 def problem_for(H, W_shards, ignore_index: int = -100, order=None, flags: int = 0,
                 strip_elems: int = 0) -> Problem:
     return Problem(H.shape[0], H.shape[1], [w.shape[0] for w in W_shards], _dtype_code(H), order,
@@ -420,9 +469,13 @@ def problem_for(H, W_shards, ignore_index: int = -100, order=None, flags: int = 
 
 
 def forward(H, W_shards: List, targets, ignore_index: int = -100, order=None, ws=None,
-            strip_elems: int = 0):
-    """(loss, lse) float32 [T] for hidden states H [T, d] and vocabulary shards W_p [V_p, d]."""
+            strip_elems: int = 0, norm: Optional[HeadNorm] = None):
+    """(loss, lse) float32 [T] for hidden states H [T, d] and vocabulary shards W_p [V_p, d].
+
+    With `norm`, H is what the norm takes and its result meets the vocabulary."""
     import torch
+    if norm is not None:
+        H = layer_norm(H, norm.gamma, norm.beta, norm.eps, norm.rms)[0]
     prob = problem_for(H, W_shards, ignore_index, order, 0, strip_elems)
     fwd_b, _ = vp_ce_workspace_size(prob)
     if ws is None:
@@ -473,9 +526,23 @@ def fold_finalize(targets, state, shard_rows: Sequence[int], ignore_index: int =
 
 
 def backward(H, W_shards: List, targets, lse, grad_loss, ignore_index: int = -100, order=None,
-             dW_shards=None, accumulate: bool = False, ws=None, strip_elems: int = 0):
-    """(dH [T, d], [dW_p [V_p, d]]) float32, recomputing the logits from the saved lse."""
+             dW_shards=None, accumulate: bool = False, ws=None, strip_elems: int = 0,
+             norm: Optional[HeadNorm] = None, dnorm=None):
+    """(dH [T, d], [dW_p [V_p, d]]) float32, recomputing the logits from the saved lse.
+
+    With `norm` (as given to `forward`): (dH, [dW_p], dgamma, dbeta) with the gradient of the
+    norm's input as dH, written over that of its result; the norm is recomputed.  dbeta is None
+    without a beta.  `dnorm`: (dgamma, dbeta) to write, or with `accumulate` to add to."""
     import torch
+    if norm is not None:
+        X = H
+        H, mean, rstd = layer_norm(X, norm.gamma, norm.beta, norm.eps, norm.rms)
+        dH, dW_shards = backward(H, W_shards, targets, lse, grad_loss, ignore_index, order, dW_shards,
+                                 accumulate, ws, strip_elems)
+        dgamma, dbeta = (None, None) if dnorm is None else dnorm
+        dH, dgamma, dbeta = layer_norm_backward(X, norm.gamma, mean, rstd, dH, norm.beta is not None, dH,
+                                                dgamma, dbeta, accumulate and dnorm is not None)
+        return dH, dW_shards, dgamma, dbeta
     flags = VP_ACCUMULATE_DW if accumulate else 0
     prob = problem_for(H, W_shards, ignore_index, order, flags, strip_elems)
     _, bwd_b = vp_ce_workspace_size(prob)

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libvpce.so")
-SOURCES = [os.path.join(CSRC, "vpce_kernels.hip"), os.path.join(CSRC, "vpce_api.cpp")]
+SOURCES = [os.path.join(CSRC, name) for name in
+           ("vpce_kernels.hip", "vpce_api.cpp", "vpce_norm.hip", "vpce_seq.hip", "vpce_head_api.cpp")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -491,6 +491,7 @@ const char* vp_status_str(vp_status s) {
     case VP_ERR_TARGET: return "a target is outside [0, V) and not ignore_index";
     case VP_ERR_HIP: return "HIP runtime or kernel launch failure";
     case VP_ERR_UNSUPPORTED: return "unsupported request";
+    case VP_ERR_VALUE: return "a parameter is outside its range";
   }
   return "unknown status";
 }
