@@ -29,12 +29,14 @@ struct NormGradArgs {
   float* dX;        // [T, d], may be dY
   float* dgamma;    // [d]
   float* dbeta;     // [d] or null
-  float* part;      // workspace
+  float* part;      // workspace: [2][norm_parts][d]
   int64_t T;
   int32_t d;
   int32_t accumulate;
 };
 
+// Rows of partial sums of dgamma (and of dbeta) that a backward writes.
+int norm_parts(int64_t T, int d);
 bool run_norm_forward(int dtype, bool rms, const NormArgs& a, hipStream_t s);
 bool run_norm_backward(int dtype, bool rms, const NormGradArgs& a, hipStream_t s);
 

@@ -24,7 +24,10 @@ vp_status validate(const vp_norm* n) {
   return VP_OK;
 }
 
-size_t norm_ws_bytes(const vp_norm*) { return 256; }
+// One row of d sums for each partial dgamma and dbeta.
+size_t norm_ws_bytes(const vp_norm* n) {
+  return 256 + 2 * (size_t)vpce::norm_parts(n->T, (int)n->d) * (size_t)n->d * 4;
+}
 
 vp_status validate(const vp_sequences* q) {
   if (!q) return VP_ERR_NULL;

@@ -1,7 +1,15 @@
-// Layer norm of the hidden states and its gradients, for gfx950 (MI355X).  Memory
-// bound: the forward reads X and writes Y, the backward reads X and dY and writes dX.
+// Layer norm of the hidden states and its gradients, for gfx950 (MI355X).
+//
+// Both directions are bound by memory: the forward reads X and writes Y once (2 e T d
+// bytes for elements of e bytes), the backward reads X and dY and writes dX once
+// ((e + 8) T d bytes).  So a row is loaded once and stays in registers, spread over W
+// wavefronts with a few 16-byte vectors of X in each lane; its sums are taken from there.
+// The variance is a second sum over the registers, around the mean, not a difference of
+// squares: a mean far above the spread costs no digits.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "vpce_head.h"
 
@@ -9,119 +17,371 @@ namespace vpce {
 
 namespace {
 
+// Element types: VEC elements per 16 bytes, as float32 and back.
 struct Half {  // bfloat16
   using storage = uint16_t;
-  __device__ static float load(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+  static constexpr int VEC = 8;
+  __device__ static void unpack(const uint4& u, float (&f)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      f[2 * k] = __uint_as_float(w[k] << 16);
+      f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+    }
+  }
   // round to nearest even; a NaN stays a NaN
-  __device__ static uint16_t store(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+  __device__ static uint32_t pack2(float lo, float hi) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    const f32x2_t v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+  }
+  __device__ static uint4 pack(const float (&f)[8]) {
+    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+  }
 };
 struct Single {
   using storage = float;
-  __device__ static float load(float f) { return f; }
-  __device__ static float store(float f) { return f; }
+  static constexpr int VEC = 4;
+  __device__ static void unpack(const uint4& u, float (&f)[4]) {
+    f[0] = __uint_as_float(u.x);
+    f[1] = __uint_as_float(u.y);
+    f[2] = __uint_as_float(u.z);
+    f[3] = __uint_as_float(u.w);
+  }
+  __device__ static uint4 pack(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
 };
 
-// Sum over a workgroup of 256 threads, the same bits in every thread.
-__device__ float block_sum(float v) {
-  __shared__ float part[4];
+// A row spread over W wavefronts, EL elements a lane: the lane's share is the vectors i,
+// i + 64 W, ... (NV of them) of the row's nvec.
+template <class E, int W, int EL>
+struct Row {
+  static constexpr int LANES = 64 * W, VEC = E::VEC, NV = EL / VEC;
+  static constexpr int ROWS = W >= 4 ? 1 : 4 / W;  // rows of a workgroup at a time
+  static constexpr int NT = LANES * ROWS;
+};
+
+// Sums N values over the W wavefronts of a row, the same bits in each lane.  red holds
+// two sets, taken in turn (`turn`), so that one barrier a sum is enough: a set is written
+// again only behind the next sum's barrier.
+template <int W, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][W], int& turn) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (part[0] + part[1]) + (part[2] + part[3]);
+  for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < N; ++k) red[turn][k][threadIdx.x >> 6] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      v[k] = red[turn][k][0];
+#pragma unroll
+      for (int w = 1; w < W; ++w) v[k] += red[turn][k][w];
+    }
+    turn ^= 1;
+  }
 }
 
-template <class E, bool RMS>
-__global__ void __launch_bounds__(256) norm_forward_kernel(NormArgs a) {
-  using S = typename E::storage;
-  const int64_t t = blockIdx.x;
-  const S* x = (const S*)a.X + t * a.d;
+template <class E, bool RMS, int W, int EL>
+__global__ void __launch_bounds__((Row<E, W, EL>::NT)) norm_forward_kernel(NormArgs a) {
+  using R = Row<E, W, EL>;
+  constexpr int VEC = R::VEC, NV = R::NV;
+  __shared__ float red[2][1][W];
+  const int lane = threadIdx.x % R::LANES, nvec = a.d / VEC;
+  const int64_t t = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / R::LANES;
+  if (R::ROWS > 1 && t >= a.T) return;  // (such rows have no barriers)
+  const uint4* x = (const uint4*)a.X + t * nvec;
+  uint4* y = (uint4*)a.Y + t * nvec;
+  int turn = 0;
+
+  float f[NV][VEC];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = lane + k * R::LANES;
+    E::unpack(i < nvec ? x[i] : make_uint4(0, 0, 0, 0), f[k]);
+  }
+  const float inv_d = 1.f / (float)a.d;
   float mean = 0.f;
   if (!RMS) {
-    float sum = 0.f;
-    for (int j = threadIdx.x; j < a.d; j += 256) sum += E::load(x[j]);
-    mean = block_sum(sum) / (float)a.d;
+    float s[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) s[0] += f[k][j];
+    row_sum<W>(s, red, turn);
+    mean = s[0] * inv_d;
   }
-  float sq = 0.f;
-  for (int j = threadIdx.x; j < a.d; j += 256) {
-    const float v = E::load(x[j]) - mean;
-    sq += v * v;
+  float s[1] = {0.f};
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const bool in = lane + k * R::LANES < nvec;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      if (!RMS) f[k][j] = in ? f[k][j] - mean : 0.f;
+      s[0] = __builtin_fmaf(f[k][j], f[k][j], s[0]);
+    }
   }
-  const float rstd = 1.f / sqrtf(block_sum(sq) / (float)a.d + a.eps);
-  for (int j = threadIdx.x; j < a.d; j += 256) {
-    float y = (E::load(x[j]) - mean) * rstd * E::load(((const S*)a.gamma)[j]);
-    if (a.beta) y += E::load(((const S*)a.beta)[j]);
-    ((S*)a.Y)[t * a.d + j] = E::store(y);
+  row_sum<W>(s, red, turn);
+  const float rstd = 1.f / sqrtf(s[0] * inv_d + a.eps);
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = lane + k * R::LANES;
+    if (i < nvec) {
+      float ga[VEC], be[VEC];
+      E::unpack(((const uint4*)a.gamma)[i], ga);
+      if (a.beta) E::unpack(((const uint4*)a.beta)[i], be);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float xh = f[k][j] * rstd;
+        ga[j] = a.beta ? __builtin_fmaf(xh, ga[j], be[j]) : xh * ga[j];
+      }
+      y[i] = E::pack(ga);
+    }
   }
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     a.rstd[t] = rstd;
     if (!RMS) a.mean[t] = mean;
   }
 }
 
-// dgamma and dbeta first (dX may overwrite dY): one thread a column.
-template <class E, bool RMS>
-__global__ void __launch_bounds__(64) norm_weight_grad_kernel(NormGradArgs a) {
-  using S = typename E::storage;
-  const int j = blockIdx.x * 64 + threadIdx.x;
-  if (j >= a.d) return;
-  float dg = 0.f, db = 0.f;
-  for (int64_t t = 0; t < a.T; ++t) {
-    const float dy = a.dY[t * a.d + j];
-    const float mean = RMS ? 0.f : a.mean[t];
-    dg += dy * ((E::load(((const S*)a.X)[t * a.d + j]) - mean) * a.rstd[t]);
-    db += dy;
+// One workgroup walks rows blockIdx.x, + gridDim.x, ... (ROWS side by side where a row
+// is a single wavefront) with the sums of dgamma and dbeta over them in registers, and
+// leaves these as one row of partial sums each (or the result, where it is alone).  The
+// order of every sum depends on the sizes alone: the same call gives the same bits.
+template <class E, bool RMS, int W, int EL>
+__global__ void __launch_bounds__((Row<E, W, EL>::NT)) norm_backward_kernel(NormGradArgs a) {
+  using R = Row<E, W, EL>;
+  constexpr int VEC = R::VEC, NV = R::NV;
+  // the next row is loaded while this one is reduced, where there are registers for it
+  constexpr bool AHEAD = EL * W <= 128;
+  __shared__ float red[2][2][W];
+  const int lane = threadIdx.x % R::LANES, group = threadIdx.x / R::LANES, nvec = a.d / VEC;
+  const int64_t step = (int64_t)gridDim.x * R::ROWS;
+  const float inv_d = 1.f / (float)a.d;
+  int turn = 0;
+
+  uint4 ga[NV];
+  float dg[NV][VEC], db[NV][VEC];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = lane + k * R::LANES;
+    ga[k] = i < nvec ? ((const uint4*)a.gamma)[i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) dg[k][j] = db[k][j] = 0.f;
   }
-  a.dgamma[j] = a.accumulate ? a.dgamma[j] + dg : dg;
-  if (a.dbeta) a.dbeta[j] = a.accumulate ? a.dbeta[j] + db : db;
+  uint4 xn[NV];
+  float4 dyn[NV][VEC / 4];
+  float mean_n = 0.f, rstd_n = 0.f;
+  auto load = [&](int64_t t) {
+    if (t >= a.T) return;
+    const uint4* x = (const uint4*)a.X + t * nvec;
+    const float4* dy = (const float4*)a.dY + t * (a.d / 4);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = lane + k * R::LANES;
+      if (i < nvec) {
+        xn[k] = x[i];
+#pragma unroll
+        for (int q = 0; q < VEC / 4; ++q) dyn[k][q] = dy[i * (VEC / 4) + q];
+      }
+    }
+    if (!RMS) mean_n = a.mean[t];
+    rstd_n = a.rstd[t];
+  };
+  int64_t t = (int64_t)blockIdx.x * R::ROWS + group;
+  if (AHEAD) load(t);
+  for (; t < a.T; t += step) {
+    if (!AHEAD) load(t);
+    uint4 xr[NV];
+    float dy[NV][VEC];
+    const float mean = mean_n, rstd = rstd_n;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      xr[k] = xn[k];
+#pragma unroll
+      for (int q = 0; q < VEC / 4; ++q) {
+        dy[k][4 * q] = dyn[k][q].x;
+        dy[k][4 * q + 1] = dyn[k][q].y;
+        dy[k][4 * q + 2] = dyn[k][q].z;
+        dy[k][4 * q + 3] = dyn[k][q].w;
+      }
+    }
+    if (AHEAD) load(t + step);
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (lane + k * R::LANES < nvec) {
+        float x[VEC], g[VEC];
+        E::unpack(xr[k], x);
+        E::unpack(ga[k], g);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float xh = (x[j] - mean) * rstd, gy = g[j] * dy[k][j];
+          s[0] += gy;
+          s[1] = __builtin_fmaf(gy, xh, s[1]);
+          dg[k][j] = __builtin_fmaf(dy[k][j], xh, dg[k][j]);
+          db[k][j] += dy[k][j];
+        }
+      }
+    row_sum<W>(s, red, turn);
+    const float c1 = RMS ? 0.f : s[0] * inv_d, c2 = s[1] * inv_d;
+    float4* dx = (float4*)a.dX + t * (a.d / 4);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = lane + k * R::LANES;
+      if (i < nvec) {
+        float x[VEC], g[VEC];
+        E::unpack(xr[k], x);
+        E::unpack(ga[k], g);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float xh = (x[j] - mean) * rstd;
+          g[j] = rstd * (g[j] * dy[k][j] - c1 - xh * c2);
+        }
+#pragma unroll
+        for (int q = 0; q < VEC / 4; ++q)
+          dx[i * (VEC / 4) + q] = make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]);
+      }
+    }
+  }
+
+  // the rows side by side first
+  if constexpr (R::ROWS > 1) {
+    __shared__ float side[R::ROWS][R::LANES][2 * VEC + 1];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        side[group][lane][j] = dg[k][j];
+        side[group][lane][VEC + j] = db[k][j];
+      }
+      __syncthreads();
+      if (group == 0)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+#pragma unroll
+          for (int r = 1; r < R::ROWS; ++r) {
+            dg[k][j] += side[r][lane][j];
+            db[k][j] += side[r][lane][VEC + j];
+          }
+      __syncthreads();
+    }
+    if (group > 0) return;
+  }
+  const bool alone = gridDim.x == 1;
+  float* out[2] = {alone ? a.dgamma : a.part + (int64_t)blockIdx.x * a.d,
+                   alone ? a.dbeta : a.part + ((int64_t)gridDim.x + blockIdx.x) * a.d};
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    if (p == 1 && !a.dbeta) break;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = lane + k * R::LANES;
+      if (i < nvec)
+#pragma unroll
+        for (int q = 0; q < VEC / 4; ++q) {
+          const float(&v)[VEC] = p ? db[k] : dg[k];
+          float4* o = (float4*)out[p] + i * (VEC / 4) + q;
+          float4 w = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+          if (alone && a.accumulate) {
+            const float4 old = *o;
+            w = make_float4(old.x + w.x, old.y + w.y, old.z + w.z, old.w + w.w);
+          }
+          *o = w;
+        }
+    }
+  }
 }
 
-template <class E, bool RMS>
-__global__ void __launch_bounds__(256) norm_input_grad_kernel(NormGradArgs a) {
-  using S = typename E::storage;
-  const int64_t t = blockIdx.x;
-  const S* x = (const S*)a.X + t * a.d;
-  const float mean = RMS ? 0.f : a.mean[t], rstd = a.rstd[t];
-  float s1 = 0.f, s2 = 0.f;
-  for (int j = threadIdx.x; j < a.d; j += 256) {
-    const float g = a.dY[t * a.d + j] * E::load(((const S*)a.gamma)[j]);
-    s1 += g;
-    s2 += g * ((E::load(x[j]) - mean) * rstd);
-  }
-  const float c1 = RMS ? 0.f : block_sum(s1) / (float)a.d;
-  const float c2 = block_sum(s2) / (float)a.d;
-  for (int j = threadIdx.x; j < a.d; j += 256) {
-    const float g = a.dY[t * a.d + j] * E::load(((const S*)a.gamma)[j]);
-    a.dX[t * a.d + j] = rstd * (g - c1 - (E::load(x[j]) - mean) * rstd * c2);
-  }
+// dgamma (blockIdx.y 0) and dbeta (1) from n rows of partial sums: 64 columns a
+// workgroup, sixteen wavefronts side by side down the rows.
+__global__ void __launch_bounds__(1024) norm_weight_grad_kernel(NormGradArgs a, int n) {
+  __shared__ float side[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x * 64 + lane;
+  const float* part = a.part + (int64_t)blockIdx.y * n * a.d;
+  float v = 0.f;
+  if (j < a.d)
+#pragma unroll 8
+    for (int r = wave; r < n; r += 16) v += part[(int64_t)r * a.d + j];
+  side[wave][lane] = v;
+  __syncthreads();
+  if (wave > 0 || j >= a.d) return;
+  for (int w = 1; w < 16; ++w) v += side[w][lane];
+  float* out = blockIdx.y ? a.dbeta : a.dgamma;
+  out[j] = a.accumulate ? out[j] + v : v;
 }
 
 bool launched_ok() { return hipGetLastError() == hipSuccess; }
 
-template <class E, bool RMS>
-bool forward(const NormArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((norm_forward_kernel<E, RMS>), dim3((unsigned)a.T), dim3(256), 0, s, a);
-  return launched_ok();
+// Runs f.run<W, EL>() for the layout of a row of d elements: W wavefronts of EL elements
+// a lane.
+template <class F>
+bool with_layout(int d, F f) {
+  if (d <= 512) return f.template run<1, 8>();
+  if (d <= 1024) return f.template run<1, 16>();
+  if (d <= 2048) return f.template run<4, 8>();
+  if (d <= 4096) return f.template run<4, 16>();
+  if (d <= 8192) return f.template run<8, 16>();
+  if (d <= 16384) return f.template run<16, 16>();
+  return f.template run<16, 32>();
 }
+
 template <class E, bool RMS>
-bool backward(const NormGradArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((norm_weight_grad_kernel<E, RMS>), dim3((unsigned)((a.d + 63) / 64)), dim3(64), 0, s, a);
-  if (!launched_ok()) return false;
-  if (a.T == 0) return true;
-  hipLaunchKernelGGL((norm_input_grad_kernel<E, RMS>), dim3((unsigned)a.T), dim3(256), 0, s, a);
-  return launched_ok();
-}
+struct Forward {
+  const NormArgs& a;
+  hipStream_t s;
+  template <int W, int EL>
+  bool run() {
+    using R = Row<E, W, EL>;
+    hipLaunchKernelGGL((norm_forward_kernel<E, RMS, W, EL>), dim3((unsigned)((a.T + R::ROWS - 1) / R::ROWS)),
+                       dim3(R::NT), 0, s, a);
+    return launched_ok();
+  }
+};
+
+template <class E, bool RMS>
+struct Backward {
+  const NormGradArgs& a;
+  hipStream_t s;
+  template <int W, int EL>
+  bool run() {
+    using R = Row<E, W, EL>;
+    const int n = norm_parts(a.T, a.d);
+    hipLaunchKernelGGL((norm_backward_kernel<E, RMS, W, EL>), dim3((unsigned)n), dim3(R::NT), 0, s, a);
+    if (!launched_ok()) return false;
+    if (n == 1) return true;
+    hipLaunchKernelGGL(norm_weight_grad_kernel, dim3((unsigned)((a.d + 63) / 64), a.dbeta ? 2u : 1u), dim3(1024), 0, s,
+                       a, n);
+    return launched_ok();
+  }
+};
 
 }  // namespace
 
+// Rows of partial sums of a backward: one a workgroup.
+int norm_parts(int64_t T, int) {
+  if (T <= 4) return 1;
+  return (int)std::min<int64_t>(T, 1024);
+}
+
 bool run_norm_forward(int dtype, bool rms, const NormArgs& a, hipStream_t s) {
-  if (dtype == VP_BF16) return rms ? forward<Half, true>(a, s) : forward<Half, false>(a, s);
-  return rms ? forward<Single, true>(a, s) : forward<Single, false>(a, s);
+  if (dtype == VP_BF16)
+    return rms ? with_layout(a.d, Forward<Half, true>{a, s})
+               : with_layout(a.d, Forward<Half, false>{a, s});
+  return rms ? with_layout(a.d, Forward<Single, true>{a, s})
+             : with_layout(a.d, Forward<Single, false>{a, s});
 }
 bool run_norm_backward(int dtype, bool rms, const NormGradArgs& a, hipStream_t s) {
-  if (dtype == VP_BF16) return rms ? backward<Half, true>(a, s) : backward<Half, false>(a, s);
-  return rms ? backward<Single, true>(a, s) : backward<Single, false>(a, s);
+  if (dtype == VP_BF16)
+    return rms ? with_layout(a.d, Backward<Half, true>{a, s})
+               : with_layout(a.d, Backward<Half, false>{a, s});
+  return rms ? with_layout(a.d, Backward<Single, true>{a, s})
+             : with_layout(a.d, Backward<Single, false>{a, s});
 }
 
 }  // namespace vpce
