@@ -226,7 +226,7 @@ vp_status vp_ce_check(const void* ws, void* stream, int64_t* bad_targets);
 
 typedef struct {
   int64_t T;      /* tokens, 0..2^23 - 256 (T == 0: nothing to do in the forward) */
-  int64_t d;      /* width, 8..32768 and a multiple of 8 (VP_ERR_SHAPE otherwise) */
+  int64_t d;      /* width, 8..16384 and a multiple of 8 (VP_ERR_SHAPE otherwise) */
   int32_t dtype;  /* vp_dtype of X, gamma, beta and Y */
   uint32_t flags; /* VP_NORM_RMS, VP_ACCUMULATE_DW */
   double eps;     /* >= 0 and finite (VP_ERR_VALUE otherwise) */

@@ -11,7 +11,7 @@
 namespace {
 
 constexpr int64_t kMaxT = (1ll << 23) - 256;  // as for vp_problem
-constexpr int64_t kMaxNormD = 32768;          // a row stays in the registers of one workgroup
+constexpr int64_t kMaxNormD = 16384;          // a row stays in the registers of one workgroup
 constexpr int64_t kMaxS = 1ll << 22;
 
 inline bool off(const void* p, uintptr_t align) { return ((uintptr_t)p & (align - 1)) != 0; }
@@ -142,8 +142,8 @@ vp_status vp_norm_backward(const vp_norm* norm, const void* X, const void* gamma
   if (st != VP_OK) return st;
   const bool rms = (norm->flags & VP_NORM_RMS) != 0;
   if ((st = check_ws(ws, ws_bytes, norm_ws_bytes(norm))) != VP_OK) return st;
-  if (!dgamma) return VP_ERR_NULL;
-  if (norm->T > 0 && (!X || !gamma || !rstd || !dY || !dX || (!rms && !mean))) return VP_ERR_NULL;
+  if (!gamma || !dgamma) return VP_ERR_NULL;
+  if (norm->T > 0 && (!X || !rstd || !dY || !dX || (!rms && !mean))) return VP_ERR_NULL;
   if (off(X, 16) || off(gamma, 16) || off(dY, 16) || off(dX, 16) || off(dgamma, 16) || off(dbeta, 16))
     return VP_ERR_ALIGN;
   if (off(rstd, 4) || (!rms && off(mean, 4))) return VP_ERR_ALIGN;

@@ -54,25 +54,27 @@ struct Single {
   }
 };
 
-// A row spread over W wavefronts, EL elements a lane: the lane's share is the vectors i,
-// i + 64 W, ... (NV of them) of the row's nvec.
-template <class E, int W, int EL>
+// A row spread over LANES lanes, EL elements each: a lane's share is the vectors i,
+// i + LANES, ... (NV of them) of the row's nvec.  Rows of up to 64 lanes lie side by side
+// in the wavefronts of a workgroup of 256.
+template <class E, int LANES_, int EL>
 struct Row {
-  static constexpr int LANES = 64 * W, VEC = E::VEC, NV = EL / VEC;
-  static constexpr int ROWS = W >= 4 ? 1 : 4 / W;  // rows of a workgroup at a time
+  static constexpr int LANES = LANES_, VEC = E::VEC, NV = EL / VEC;
+  static constexpr int W = LANES > 64 ? LANES / 64 : 1;
+  static constexpr int ROWS = LANES <= 64 ? 256 / LANES : 1;  // rows of a workgroup at a time
   static constexpr int NT = LANES * ROWS;
 };
 
-// Sums N values over the W wavefronts of a row, the same bits in each lane.  red holds
-// two sets, taken in turn (`turn`), so that one barrier a sum is enough: a set is written
+// Sums N values over the LANES lanes of a row, the same bits in each.  red holds two
+// sets, taken in turn (`turn`), so that one barrier a sum is enough: a set is written
 // again only behind the next sum's barrier.
-template <int W, int N>
+template <int LANES, int N, int W>
 __device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][W], int& turn) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1)
+  for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1)
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
-  if constexpr (W > 1) {
+  if constexpr (LANES > 64) {
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
       for (int k = 0; k < N; ++k) red[turn][k][threadIdx.x >> 6] = v[k];
@@ -87,11 +89,11 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][W], int& 
   }
 }
 
-template <class E, bool RMS, int W, int EL>
-__global__ void __launch_bounds__((Row<E, W, EL>::NT)) norm_forward_kernel(NormArgs a) {
-  using R = Row<E, W, EL>;
+template <class E, bool RMS, int LANES, int EL>
+__global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(NormArgs a) {
+  using R = Row<E, LANES, EL>;
   constexpr int VEC = R::VEC, NV = R::NV;
-  __shared__ float red[2][1][W];
+  __shared__ float red[2][1][R::W];
   const int lane = threadIdx.x % R::LANES, nvec = a.d / VEC;
   const int64_t t = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / R::LANES;
   if (R::ROWS > 1 && t >= a.T) return;  // (such rows have no barriers)
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__((Row<E, W, EL>::NT)) norm_forward_kernel(NormA
     for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) s[0] += f[k][j];
-    row_sum<W>(s, red, turn);
+    row_sum<LANES>(s, red, turn);
     mean = s[0] * inv_d;
   }
   float s[1] = {0.f};
@@ -126,7 +128,7 @@ __global__ void __launch_bounds__((Row<E, W, EL>::NT)) norm_forward_kernel(NormA
       s[0] = __builtin_fmaf(f[k][j], f[k][j], s[0]);
     }
   }
-  row_sum<W>(s, red, turn);
+  row_sum<LANES>(s, red, turn);
   const float rstd = 1.f / sqrtf(s[0] * inv_d + a.eps);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -153,13 +155,13 @@ __global__ void __launch_bounds__((Row<E, W, EL>::NT)) norm_forward_kernel(NormA
 // is a single wavefront) with the sums of dgamma and dbeta over them in registers, and
 // leaves these as one row of partial sums each (or the result, where it is alone).  The
 // order of every sum depends on the sizes alone: the same call gives the same bits.
-template <class E, bool RMS, int W, int EL>
-__global__ void __launch_bounds__((Row<E, W, EL>::NT)) norm_backward_kernel(NormGradArgs a) {
-  using R = Row<E, W, EL>;
+template <class E, bool RMS, int LANES, int EL>
+__global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(NormGradArgs a) {
+  using R = Row<E, LANES, EL>;
   constexpr int VEC = R::VEC, NV = R::NV;
   // the next row is loaded while this one is reduced, where there are registers for it
-  constexpr bool AHEAD = EL * W <= 128;
-  __shared__ float red[2][2][W];
+  constexpr bool AHEAD = EL * LANES <= 8192;
+  __shared__ float red[2][2][R::W];
   const int lane = threadIdx.x % R::LANES, group = threadIdx.x / R::LANES, nvec = a.d / VEC;
   const int64_t step = (int64_t)gridDim.x * R::ROWS;
   const float inv_d = 1.f / (float)a.d;
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__((Row<E, W, EL>::NT)) norm_backward_kernel(Norm
           db[k][j] += dy[k][j];
         }
       }
-    row_sum<W>(s, red, turn);
+    row_sum<LANES>(s, red, turn);
     const float c1 = RMS ? 0.f : s[0] * inv_d, c2 = s[1] * inv_d;
     float4* dx = (float4*)a.dX + t * (a.d / 4);
 #pragma unroll
@@ -318,27 +320,58 @@ __global__ void __launch_bounds__(1024) norm_weight_grad_kernel(NormGradArgs a, 
 
 bool launched_ok() { return hipGetLastError() == hipSuccess; }
 
-// Runs f.run<W, EL>() for the layout of a row of d elements: W wavefronts of EL elements
-// a lane.
+// Run f.run<LANES, EL>() for the layout of a row of d elements.
+//
+// Forward: 32 bytes of X a lane (64 for bfloat16 rows of 2049 to 4096 elements).  Fewer
+// bytes a lane leave more of a workgroup to its two sums, more leave fewer loads in
+// flight, and what counts as few differs by type.  GB/s, bfloat16 / float32:
+//   T = 65536, d = 1000: 64 x 16 5520 / 5020, 128 x 8 4720 / 5630
+//   T = 30000, d = 2048: 128 x 16 5430 / 5610, 256 x 8 4710 / 5860
+//   T = 32768, d = 2880: 128 x 32 5460 / 5480, 256 x 16 5150 / 5870, 512 x 8 4050 / 6010
+//   T = 16384, d = 4096: 128 x 32 5330 / 5370, 256 x 16 5540 / 5730, 512 x 8 4860 / 5950
+//   T = 16384, d = 7168: 256 x 32 5240 / 5480, 512 x 16 5330 / 5790, 1024 x 8 4440 / 5880
+template <class E, class F>
+bool forward_layout(int d, F&& f) {
+  if (d <= 64) return f.template run<8, 8>();
+  if (d <= 128) return f.template run<16, 8>();
+  if (d <= 256) return f.template run<32, 8>();
+  if (d <= 512) return f.template run<64, 8>();
+  if constexpr (E::VEC == 8) {
+    if (d <= 1024) return f.template run<64, 16>();
+    if (d <= 2048) return f.template run<128, 16>();
+    if (d <= 4096) return f.template run<128, 32>();
+    if (d <= 8192) return f.template run<512, 16>();
+  } else {
+    if (d <= 1024) return f.template run<128, 8>();
+    if (d <= 2048) return f.template run<256, 8>();
+    if (d <= 4096) return f.template run<512, 8>();
+    if (d <= 8192) return f.template run<1024, 8>();
+  }
+  return f.template run<1024, 16>();
+}
+
+// Backward: as few wavefronts as hold the row with its sums and the next row in registers.
 template <class F>
-bool with_layout(int d, F f) {
-  if (d <= 512) return f.template run<1, 8>();
-  if (d <= 1024) return f.template run<1, 16>();
-  if (d <= 2048) return f.template run<4, 8>();
-  if (d <= 4096) return f.template run<4, 16>();
-  if (d <= 8192) return f.template run<8, 16>();
-  if (d <= 16384) return f.template run<16, 16>();
-  return f.template run<16, 32>();
+bool backward_layout(int d, F&& f) {
+  if (d <= 64) return f.template run<8, 8>();
+  if (d <= 128) return f.template run<16, 8>();
+  if (d <= 256) return f.template run<32, 8>();
+  if (d <= 512) return f.template run<64, 8>();
+  if (d <= 1024) return f.template run<64, 16>();
+  if (d <= 2048) return f.template run<256, 8>();
+  if (d <= 4096) return f.template run<256, 16>();
+  if (d <= 8192) return f.template run<512, 16>();
+  return f.template run<1024, 16>();
 }
 
 template <class E, bool RMS>
 struct Forward {
   const NormArgs& a;
   hipStream_t s;
-  template <int W, int EL>
+  template <int LANES, int EL>
   bool run() {
-    using R = Row<E, W, EL>;
-    hipLaunchKernelGGL((norm_forward_kernel<E, RMS, W, EL>), dim3((unsigned)((a.T + R::ROWS - 1) / R::ROWS)),
+    using R = Row<E, LANES, EL>;
+    hipLaunchKernelGGL((norm_forward_kernel<E, RMS, LANES, EL>), dim3((unsigned)((a.T + R::ROWS - 1) / R::ROWS)),
                        dim3(R::NT), 0, s, a);
     return launched_ok();
   }
@@ -348,11 +381,11 @@ template <class E, bool RMS>
 struct Backward {
   const NormGradArgs& a;
   hipStream_t s;
-  template <int W, int EL>
+  template <int LANES, int EL>
   bool run() {
-    using R = Row<E, W, EL>;
+    using R = Row<E, LANES, EL>;
     const int n = norm_parts(a.T, a.d);
-    hipLaunchKernelGGL((norm_backward_kernel<E, RMS, W, EL>), dim3((unsigned)n), dim3(R::NT), 0, s, a);
+    hipLaunchKernelGGL((norm_backward_kernel<E, RMS, LANES, EL>), dim3((unsigned)n), dim3(R::NT), 0, s, a);
     if (!launched_ok()) return false;
     if (n == 1) return true;
     hipLaunchKernelGGL(norm_weight_grad_kernel, dim3((unsigned)((a.d + 63) / 64), a.dbeta ? 2u : 1u), dim3(1024), 0, s,
@@ -361,27 +394,47 @@ struct Backward {
   }
 };
 
+// Workgroups of a backward, each with one row of partial sums.  Rows are walked by one
+// workgroup a CU, or two where a workgroup's rows hold 2048 elements: with the next row on
+// its way that keeps the memory busy, and more of them only add partial sums to write and
+// read (T = 32768, d = 2880, bfloat16: 256 workgroups 171 us, 512 173, 1024 196; float32
+// 195, 212, 231; T = 30000, d = 1200: 113, 75, 72 and 110, 80, 84).  No workgroup sums more
+// than 1024 rows in one chain.  Up to four rounds of rows one workgroup does it all and
+// the second launch is saved (T = 4, d = 4096: 9.2 us for the call instead of 12.3; T = 16
+// in one workgroup 20.4).
+struct Parts {
+  int rows, n;
+  template <int LANES, int EL>
+  bool run() {
+    rows = Row<Half, LANES, EL>::ROWS;
+    n = LANES * EL * rows == 2048 ? 512 : 256;
+    return true;
+  }
+};
+
 }  // namespace
 
-// Rows of partial sums of a backward: one a workgroup.
-int norm_parts(int64_t T, int) {
-  if (T <= 4) return 1;
-  return (int)std::min<int64_t>(T, 1024);
+int norm_parts(int64_t T, int d) {
+  Parts p{};
+  backward_layout(d, p);
+  const int64_t rounds = (T + p.rows - 1) / p.rows;
+  if (rounds <= 4) return 1;
+  return (int)std::max<int64_t>(std::min<int64_t>(rounds, p.n), (rounds + 1023) / 1024);
 }
 
 bool run_norm_forward(int dtype, bool rms, const NormArgs& a, hipStream_t s) {
   if (dtype == VP_BF16)
-    return rms ? with_layout(a.d, Forward<Half, true>{a, s})
-               : with_layout(a.d, Forward<Half, false>{a, s});
-  return rms ? with_layout(a.d, Forward<Single, true>{a, s})
-             : with_layout(a.d, Forward<Single, false>{a, s});
+    return rms ? forward_layout<Half>(a.d, Forward<Half, true>{a, s})
+               : forward_layout<Half>(a.d, Forward<Half, false>{a, s});
+  return rms ? forward_layout<Single>(a.d, Forward<Single, true>{a, s})
+             : forward_layout<Single>(a.d, Forward<Single, false>{a, s});
 }
 bool run_norm_backward(int dtype, bool rms, const NormGradArgs& a, hipStream_t s) {
   if (dtype == VP_BF16)
-    return rms ? with_layout(a.d, Backward<Half, true>{a, s})
-               : with_layout(a.d, Backward<Half, false>{a, s});
-  return rms ? with_layout(a.d, Backward<Single, true>{a, s})
-             : with_layout(a.d, Backward<Single, false>{a, s});
+    return rms ? backward_layout(a.d, Backward<Half, true>{a, s})
+               : backward_layout(a.d, Backward<Half, false>{a, s});
+  return rms ? backward_layout(a.d, Backward<Single, true>{a, s})
+             : backward_layout(a.d, Backward<Single, false>{a, s});
 }
 
 }  // namespace vpce

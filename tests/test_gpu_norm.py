@@ -1,7 +1,7 @@
 """Layer norm and its gradients on the GPU against the plain float64 form.
 
-Bounds, with u = 2^-24 and sums of at most DEPTH additions in a chain (a row of 32768 over 256
-threads, then the threads; fewer in every other layout), so that a float32 sum of x_k is off by at
+Bounds, with u = 2^-24 and sums of a row in chains of at most DEPTH additions (a lane's
+elements, then the lanes), so that a float32 sum of x_k is off by at
 most DEPTH u sum |x_k|:
 * mean: DEPTH u mean|x|; the variance around a mean that is off by e gains e^2, and its own sum
   and squares (DEPTH + 4) u, so rstd is off by half of that and 3 u, relative;
@@ -73,8 +73,10 @@ def _check_backward(X, gamma, mean, rstd, dY, got, base=None):
         _within(dbeta, db + old[1], (ROWS(T) + 1) * U * (dy.abs().sum(0) + abs(old[1])) + 1e-44, "dbeta")
 
 
-SIZES = [(1, 8), (1, 4096), (2, 32768), (3, 40), (5, 1000), (37, 2880), (130, 264), (257, 512), (64, 7168),
-         (9, 16384), (700, 1032), (4100, 64), (1500, 2056), (33, 8200), (2049, 128)]
+# every layout of a row, its widest and a width that leaves part of it empty
+SIZES = [(1, 8), (1, 4096), (2, 16384), (3, 40), (5, 1000), (37, 2880), (130, 264), (257, 512), (64, 7168),
+         (9, 16384), (700, 1032), (4100, 64), (1500, 2056), (33, 8200), (2049, 128), (70, 256), (45, 776), (19, 1024), (23, 2048), (31, 3336),
+         (3, 5000), (6, 8192), (150, 72), (5, 9000)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])

@@ -66,7 +66,7 @@ def _pol_bwd(seq=None, pol=None, **over):
 
 BAD_NORMS = [
     (dict(T=-1), vp.VP_ERR_SHAPE), (dict(T=2 ** 23 - 255), vp.VP_ERR_SHAPE), (dict(d=0), vp.VP_ERR_SHAPE),
-    (dict(d=4), vp.VP_ERR_SHAPE), (dict(d=60), vp.VP_ERR_SHAPE), (dict(d=32776), vp.VP_ERR_SHAPE),
+    (dict(d=4), vp.VP_ERR_SHAPE), (dict(d=60), vp.VP_ERR_SHAPE), (dict(d=16392), vp.VP_ERR_SHAPE),
     (dict(dtype=2), vp.VP_ERR_DTYPE), (dict(eps=-1e-6), vp.VP_ERR_VALUE), (dict(eps=math.nan), vp.VP_ERR_VALUE),
     (dict(eps=math.inf), vp.VP_ERR_VALUE),
 ]
