@@ -47,7 +47,17 @@ struct SeqArgs {
   int64_t ignore_index;
   int32_t T, S;
   int32_t mean;
+  int32_t chunk;  // tokens of a chunk
+  double* part;   // workspace: [slots][sums]; the forwards' alone
 };
+
+// How the tokens of a forward are cut, and its partial sums.
+struct SeqPlan {
+  int32_t chunk, chunks;
+  int64_t slots;
+};
+SeqPlan seq_plan(int T, int S);
+constexpr int kMaxSeqSums = 3;  // of one slot
 
 struct PrefArgs {
   SeqArgs q;

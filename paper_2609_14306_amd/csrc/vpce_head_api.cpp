@@ -35,7 +35,9 @@ vp_status validate(const vp_sequences* q) {
   return VP_OK;
 }
 
-size_t seq_ws_bytes(const vp_sequences*) { return 256; }
+size_t seq_ws_bytes(const vp_sequences* q) {
+  return 256 + (size_t)vpce::seq_plan((int)q->T, (int)q->S).slots * vpce::kMaxSeqSums * sizeof(double);
+}
 
 vp_status validate(const vp_preference* p) {
   if (!p) return VP_ERR_NULL;
@@ -65,7 +67,8 @@ vp_status check_tokens(const vp_sequences* q, const int32_t* start, const int64_
   return off(start, 4) || off(targets, 8) ? VP_ERR_ALIGN : VP_OK;
 }
 
-vpce::SeqArgs seq_args(const vp_sequences* q, const int32_t* start, const int64_t* targets) {
+vpce::SeqArgs seq_args(const vp_sequences* q, const int32_t* start, const int64_t* targets,
+                       void* ws = nullptr) {
   vpce::SeqArgs a;
   a.start = start;
   a.targets = targets;
@@ -73,6 +76,8 @@ vpce::SeqArgs seq_args(const vp_sequences* q, const int32_t* start, const int64_
   a.T = (int32_t)q->T;
   a.S = (int32_t)q->S;
   a.mean = (q->flags & VP_SEQ_MEAN) != 0;
+  a.chunk = vpce::seq_plan(a.T, a.S).chunk;
+  a.part = (double*)ws;
   return a;
 }
 
@@ -185,7 +190,7 @@ vp_status vp_pref_forward(const vp_sequences* seq, const vp_preference* pref, co
   if (off(loss, 4) || off(ref_loss, 4) || off(pair_loss, 4) || off(reward, 4) || off(coef, 4))
     return VP_ERR_ALIGN;
   vpce::PrefArgs a;
-  a.q = seq_args(seq, start, targets);
+  a.q = seq_args(seq, start, targets, ws);
   a.loss = loss;
   a.ref = ref_loss;
   a.kind = pref->kind;
@@ -224,6 +229,7 @@ vp_status vp_policy_forward(const vp_sequences* seq, const vp_policy* policy, co
   if ((st = check_ws(ws, ws_bytes, seq_ws_bytes(seq))) != VP_OK) return st;
   if (seq->S > 0 && (!seq_loss || !seq_kl || !clipped || !tokens)) return VP_ERR_NULL;
   if (off(seq_loss, 4) || off(seq_kl, 4) || off(clipped, 4) || off(tokens, 4)) return VP_ERR_ALIGN;
+  a.q.part = (double*)ws;
   a.seq_loss = seq_loss;
   a.seq_kl = seq_kl;
   a.clipped = clipped;
