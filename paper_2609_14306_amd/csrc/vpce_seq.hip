@@ -7,67 +7,120 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "vpce_head.h"
 
 namespace vpce {
 
 namespace {
 
-constexpr int kRound = 256;  // tokens that a wavefront takes at a time, four a lane
+constexpr int kWaves = 4096;  // wavefronts that fill the chip: four on each of 1024 SIMDs
 
 __device__ __forceinline__ int lane_id() { return threadIdx.x & 63; }
 
+// v of another lane through the data-parallel path (CTRL: the lane selection), 0 where
+// the selection has no lane or ROWS leaves the lane's row of 16 out.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int lane_move(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double lane_move(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)lane_move<CTRL, ROWS>((int)(uint32_t)u);
+  const uint32_t hi = (uint32_t)lane_move<CTRL, ROWS>((int)(uint32_t)(u >> 32));
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e;                            // lane ^ 1, lane ^ 2
+constexpr int kHalfMirror = 0x141, kMirror = 0x140;                    // 7 - lane in 8, 15 - lane in 16
+constexpr int kUp1 = 0x111, kUp2 = 0x112, kUp4 = 0x114, kUp8 = 0x118;  // lane - n in 16
+constexpr int kRowEnd = 0x142, kHalfEnd = 0x143;  // last lane of the row / the half in front
+
+__device__ __forceinline__ double lane_read(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// Sum over a wavefront, the same in every lane.
 template <int N>
 __device__ __forceinline__ void wave_sum(double (&v)[N]) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1)
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
-}
-
-// The sequence of token t: the last one whose start is not behind it, S for tokens
-// behind all of them, -1 for tokens before.  One wavefront, 64 probes at a time; for any
-// offsets it ends and the answer is in -1..S.
-__device__ __forceinline__ int sequence_of(const SeqArgs& q, int t) {
-  if (q.S == 0) return -1;
-  int lo = 0, n = q.S + 1;  // start[i] <= t for i < lo, start[i] > t for i >= lo + n
-  while (n > 64) {
-    const int step = (n + 63) / 64, i = lo + (lane_id() + 1) * step - 1;
-    const int c = __popcll(__ballot(i < lo + n && q.start[min(i, q.S)] <= t));
-    lo += c * step;
-    n = min(step - 1, n - c * step);
+  for (int k = 0; k < N; ++k) {
+    v[k] += lane_move<kSwap1>(v[k]);
+    v[k] += lane_move<kSwap2>(v[k]);
+    v[k] += lane_move<kHalfMirror>(v[k]);
+    v[k] += lane_move<kMirror>(v[k]);
+    v[k] = (lane_read(v[k], 0) + lane_read(v[k], 16)) + (lane_read(v[k], 32) + lane_read(v[k], 48));
   }
-  const int i = lo + lane_id();
-  return lo + __popcll(__ballot(lane_id() < n && q.start[min(i, q.S)] <= t)) - 1;
 }
 
-// The sequences of up to 64 tokens in order, one a lane, the first of them at or behind
-// sequence s: counts the offsets behind start[s] that are not behind the lane's token.
-// `last` is the last lane's token.  For any offsets it ends and the answer is in s..S.
-__device__ __forceinline__ int sequences_from(const SeqArgs& q, int s, int t, int last) {
-  int mine = s;
-  for (int first = s + 1; first <= q.S; first += 64) {
-    const int i = first + lane_id();
-    const int o = i <= q.S ? q.start[i] : INT32_MAX;
-    int lo = 0, hi = 64;  // o of lanes < lo is not behind t, o of lanes >= hi is
+// Sums over the lanes from the last head at or in front of each lane up to it.
+template <int CTRL, int ROWS, int N>
+__device__ __forceinline__ void scan_step(double (&v)[N], int& head) {
+  const int h = lane_move<CTRL, ROWS>(head);
 #pragma unroll
-    for (int k = 0; k < 7; ++k) {
-      const int mid = (lo + hi) >> 1, at = __shfl(o, mid & 63);
-      if (lo < hi) {
-        if (at <= t)
-          lo = mid + 1;
-        else
-          hi = mid;
-      }
+  for (int k = 0; k < N; ++k) {
+    const double w = lane_move<CTRL, ROWS>(v[k]);
+    v[k] = head ? v[k] : v[k] + w;
+  }
+  head |= h;
+}
+template <int N>
+__device__ __forceinline__ void segmented_scan(double (&v)[N], int head) {
+  scan_step<kUp1, 0xf>(v, head);
+  scan_step<kUp2, 0xf>(v, head);
+  scan_step<kUp4, 0xf>(v, head);
+  scan_step<kUp8, 0xf>(v, head);
+  scan_step<kRowEnd, 0xa>(v, head);
+  scan_step<kHalfEnd, 0xc>(v, head);
+}
+
+// 64 consecutive offsets, one a lane: start[base + lane] (INT32_MAX behind the last).
+// The sequence of a token t is the last one whose start is not behind it, S for tokens
+// behind all of them and -1 for tokens before.  Whatever the offsets are, every walk
+// below ends and every sequence it names is in -1..S.
+struct Window {
+  int base, o;
+  __device__ __forceinline__ void load(const SeqArgs& q) {
+    o = base + lane_id() <= q.S && q.S > 0 ? q.start[base + lane_id()] : INT32_MAX;
+  }
+  // Moves to where token t is, 64 probes at a time; its sequence.
+  __device__ __forceinline__ int open(const SeqArgs& q, int t) {
+    int lo = 0, n = q.S + 1;  // start[i] <= t for i < lo, start[i] > t for i >= lo + n
+    while (n > 64) {
+      const int step = (n + 63) / 64, i = lo + (lane_id() + 1) * step - 1;
+      const int c = __popcll(__ballot(i < lo + n && q.start[min(i, q.S)] <= t));
+      lo += c * step;
+      n = min(step - 1, n - c * step);
     }
-    mine += lo;
-    if (__shfl(o, 63) > last) break;
+    base = lo;
+    load(q);
+    return base - 1 + __popcll(__ballot(o <= t));
   }
-  return mine;
-}
-
-// End of sequence s: its tokens are in front of it (tokens before the first: s = -1).
-__device__ __forceinline__ int end_of(const SeqArgs& q, int s) { return s < q.S ? q.start[s + 1] : INT32_MAX; }
+  // End of sequence s, the last one looked up.
+  __device__ __forceinline__ int end(const SeqArgs& q, int s) const {
+    const int i = s + 1 - base;
+    if (i >= 0 && i < 64) return __builtin_amdgcn_readlane(o, i);
+    return s < q.S ? q.start[s + 1] : INT32_MAX;
+  }
+  // Sequences of the tokens first..last, one a lane (the lanes behind get last's), which
+  // are not in front of a token looked up before.
+  __device__ __forceinline__ int walk(const SeqArgs& q, int first, int last) {
+    const int t = min(first + lane_id(), last);
+    int s = base - 1;
+    for (;;) {
+      s += __popcll(__ballot(o <= first));
+      for (uint64_t m = __ballot(o > first && o <= last); m; m &= m - 1)
+        s += __builtin_amdgcn_readlane(o, __builtin_ctzll(m)) <= t;
+      if (__builtin_amdgcn_readlane(o, 63) > last) return s;
+      base += 64;
+      load(q);
+    }
+  }
+};
 
 // Partial sums.  The tokens are cut into chunks of q.chunk, a wavefront each, and chunk c
 // leaves its part of sequence s in slot c + s: walking the tokens, every step to another
@@ -75,9 +128,9 @@ __device__ __forceinline__ int end_of(const SeqArgs& q, int s) { return s < q.S 
 // are enough.
 //
 // The sums of the sequence that a chunk is in stay spread over the lanes as long as it
-// lasts.  Where a round of tokens holds an end, its tokens go through a segmented scan, 64
-// at a time, which takes the same time for one end or 63.
-template <class Op>
+// lasts.  64 tokens that hold an end go through a segmented scan, which takes the same
+// time for one end or 63.  J: tokens a lane loads at a time, the next ones on their way.
+template <int J, class Op>
 __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
   constexpr int K = Op::K;
   const SeqArgs& q = op.a.q;
@@ -93,33 +146,42 @@ __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
   double acc[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) acc[k] = 0.0;
-  int s = -2, end = 0;  // the sequence that the walk is in, and its end
-  for (int base = t0; base < t1; base += kRound) {
-    typename Op::Raw raw[4];
+  typename Op::Raw raw[J], next[J];
+  auto load = [&](int base) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) op.load(raw[j], min(base + 64 * j + lane, t1 - 1));
-    if (s == -2) {  // (behind the first loads)
-      s = sequence_of(q, t0);
-      end = end_of(q, s);
+    for (int j = 0; j < J; ++j) op.load(next[j], min(base + 64 * j + lane, t1 - 1));
+  };
+  load(t0);
+  Window w;
+  int s = w.open(q, t0), end = w.end(q, s);  // the sequence that the walk is in, and its end
+  for (int base = t0; base < t1; base += 64 * J) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) raw[j] = next[j];
+    if (base + 64 * J < t1) load(base + 64 * J);
+    if (min(base + 64 * J, t1) <= end) {
+      if (s >= 0 && s < q.S)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+          if (base + 64 * j + lane < t1) op.add(acc, raw[j], s);
+      continue;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int b = base + 64 * j, e = min(b + 64, t1);
-      if (b >= t1) break;
-      const bool in = b + lane < e;
+#pragma unroll 1
+    for (int b = base; b < min(base + 64 * J, t1); b += 64) {
+      const int e = min(b + 64, t1);
+      typename Op::Raw r = raw[0];
+      if (J > 1) op.load(r, min(b + lane, t1 - 1));
       if (e <= end) {
-        if (in && s >= 0 && s < q.S) op.add(acc, raw[j], s);
+        if (b + lane < e && s >= 0 && s < q.S) op.add(acc, r, s);
         continue;
       }
-      // an end inside: close the lanes' sums and scan
       wave_sum(acc);
-      const int mine = sequences_from(q, s, min(b + lane, e - 1), e - 1);
+      const int mine = w.walk(q, b, e - 1);
       double v[K];
 #pragma unroll
       for (int k = 0; k < K; ++k) v[k] = 0.0;
-      if (in && mine >= 0 && mine < q.S) op.add(v, raw[j], mine);
-      const int up = __shfl_up(mine, 1), next = __shfl_down(mine, 1);  // (every lane takes part)
-      bool head = mine != (lane ? up : s);
+      if (b + lane < e && mine >= 0 && mine < q.S) op.add(v, r, mine);
+      const int up = __shfl_up(mine, 1), down = __shfl_down(mine, 1);
+      const bool head = mine != (lane ? up : s);
       if (lane == 0) {
         if (head)
           put(s, acc);
@@ -127,24 +189,15 @@ __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
 #pragma unroll
           for (int k = 0; k < K; ++k) v[k] += acc[k];
       }
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const bool h = __shfl_up((int)head, o);
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const double w = __shfl_up(v[k], o);
-          if (lane >= o && !head) v[k] += w;
-        }
-        if (lane >= o) head |= h;
-      }
-      if (lane < 63 && next != mine) put(mine, v);
+      segmented_scan(v, (int)head);
+      if (lane < 63 && down != mine) put(mine, v);
       // the last lane's sequence goes on
-      s = __shfl(mine, 63);
-      end = end_of(q, s);
+      s = __builtin_amdgcn_readlane(mine, 63);
+      end = w.end(q, s);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const double w = __shfl(v[k], 63);
-        acc[k] = lane ? 0.0 : w;
+        const double x = lane_read(v[k], 63);
+        acc[k] = lane ? 0.0 : x;
       }
     }
   }
@@ -237,6 +290,33 @@ struct PrefOp {
   }
 };
 
+// e^x and e^x - 1: x = n ln 2 + r with |r| <= 0.3466, p = e^r - 1 by its series up to
+// r^13 / 13! (the next term is below 2^-59 r), e^x = 2^n (1 + p).  e^x - 1 is p itself for
+// n = 0 and loses at most two bits to the difference otherwise.  Half the instructions of
+// the library's exp and expm1, which also carry their answers to the last bit.
+__device__ __forceinline__ void exp_both(double x, double& e, double& em1) {
+  const double y = fmin(fmax(x, -1100.0), 1100.0);
+  const double n = rint(y * 1.4426950408889634);
+  double r = fma(n, -0.6931471805599453, y);
+  r = fma(n, -2.3190468138462996e-17, r);
+  double p = 1.0 / 6227020800.0;
+  p = fma(p, r, 1.0 / 479001600.0);
+  p = fma(p, r, 1.0 / 39916800.0);
+  p = fma(p, r, 1.0 / 3628800.0);
+  p = fma(p, r, 1.0 / 362880.0);
+  p = fma(p, r, 1.0 / 40320.0);
+  p = fma(p, r, 1.0 / 5040.0);
+  p = fma(p, r, 1.0 / 720.0);
+  p = fma(p, r, 1.0 / 120.0);
+  p = fma(p, r, 1.0 / 24.0);
+  p = fma(p, r, 1.0 / 6.0);
+  p = fma(p, r, 0.5);
+  p = fma(p * r, r, r);
+  e = ldexp(1.0 + p, (int)n);
+  em1 = n == 0.0 ? p : e - 1.0;
+  if (!(x == x)) e = em1 = x;
+}
+
 // The policy loss of one token and its slope in loss_t.
 struct PolicyToken {
   double loss, kl, slope;
@@ -259,14 +339,17 @@ __device__ __forceinline__ PolicyToken policy_token(const PolicyArgs& a, const P
   // (a NaN loss makes x a NaN without an old loss, too)
   const double x = a.old ? (double)t.old - nll : (nll == nll ? 0.0 : nll);
   r.clipped = adv > 0.0 ? x > a.log_high : adv < 0.0 ? x < a.log_low : false;
-  const double rho = a.old ? exp(x) : 1.0 + x;
+  double rho = 1.0 + x, unused;
+  if (a.old) exp_both(x, rho, unused);
   // no advantage: 0 also where rho is infinite
   const double gain = adv == 0.0 ? (x == x ? 0.0 : x) : rho * adv;
   r.loss = r.clipped ? -((adv > 0.0 ? a.high : a.low) * adv) : -gain;
   r.slope = r.clipped ? 0.0 : gain;
   r.kl = 0.0;
   if (a.ref) {
-    const double q = nll - (double)t.ref, em1 = expm1(q);
+    const double q = nll - (double)t.ref;
+    double em1;
+    exp_both(q, unused, em1);
     r.kl = em1 == __builtin_inf() ? em1 : em1 - q;  // (q infinite: no difference of infinities)
     if (a.kl_coef > 0.0) {
       r.loss += a.kl_coef * r.kl;
@@ -306,10 +389,10 @@ struct PolicyOp {
   }
 };
 
-template <class Op, class Args>
+template <int J, class Op, class Args>
 __global__ void __launch_bounds__(256) chunk_kernel(Args args) {
   const Op op{args};
-  chunk_sums(op, __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  chunk_sums<J>(op, __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)));
 }
 template <class Op, class Args, int LANES>
 __global__ void __launch_bounds__(256) finish_kernel(Args args) {
@@ -321,12 +404,12 @@ __global__ void __launch_bounds__(256) finish_kernel(Args args) {
 template <class Op, class Args>
 __global__ void __launch_bounds__(1024) small_kernel(Args args) {
   const Op op{args};
-  chunk_sums(op, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  chunk_sums<1>(op, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
   __syncthreads();
   for (int unit = threadIdx.x; unit < args.q.S / Op::PER_UNIT; unit += 1024) op.template finish<1>(unit);
 }
 
-// Gradients: a round of tokens a wavefront.
+// Gradients: J tokens a lane.
 struct PrefGrad {
   SeqArgs q;
   const float* coef;
@@ -350,25 +433,26 @@ struct PolicyGrad {
                    policy_token(a, r, (double)(a.per_token ? r.adv : a.adv[s])).slope);
   }
 };
-template <class Op>
+template <int J, class Op>
 __global__ void __launch_bounds__(256) grad_kernel(Op op) {
   const SeqArgs& q = op.q;
   const int lane = lane_id();
-  const int base = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) * kRound;
+  const int base = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * J);
   if (base >= q.T) return;
-  typename Op::Raw raw[4];
+  typename Op::Raw raw[J];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) op.load(raw[j], min(base + 64 * j + lane, q.T - 1));
-  int s = sequence_of(q, base), end = end_of(q, s);
+  for (int j = 0; j < J; ++j) op.load(raw[j], min(base + 64 * j + lane, q.T - 1));
+  Window w;
+  int s = w.open(q, base), end = w.end(q, s);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < J; ++j) {
     const int b = base + 64 * j, e = min(b + 64, q.T);
     if (b >= q.T) break;
     int mine = s;
     if (e > end) {
-      mine = sequences_from(q, s, min(b + lane, e - 1), e - 1);
-      s = __shfl(mine, 63);
-      end = end_of(q, s);
+      mine = w.walk(q, b, e - 1);
+      s = __builtin_amdgcn_readlane(mine, 63);
+      end = w.end(q, s);
     }
     if (b + lane < e) {
       const bool counts = mine >= 0 && mine < q.S && raw[j].target != q.ignore_index;
@@ -388,7 +472,11 @@ bool forward(const Args& a, hipStream_t s) {
     hipLaunchKernelGGL((small_kernel<Op, Args>), dim3(1), dim3(1024), 0, s, a);
     return launched_ok();
   }
-  hipLaunchKernelGGL((chunk_kernel<Op, Args>), dim3((unsigned)(p.chunks + 3) / 4), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)(p.chunks + 3) / 4);
+  if (p.chunk <= 128)
+    hipLaunchKernelGGL((chunk_kernel<1, Op, Args>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((chunk_kernel<4, Op, Args>), grid, dim3(256), 0, s, a);
   if (!launched_ok()) return false;
   const int units = q.S / Op::PER_UNIT;
   if (units <= 16384)
@@ -399,9 +487,12 @@ bool forward(const Args& a, hipStream_t s) {
 }
 template <class Op>
 bool backward(const Op& op, hipStream_t s) {
-  if (op.q.T == 0) return true;
-  const unsigned rounds = (unsigned)(op.q.T + kRound - 1) / kRound;
-  hipLaunchKernelGGL((grad_kernel<Op>), dim3((rounds + 3) / 4), dim3(256), 0, s, op);
+  const int T = op.q.T;
+  if (T == 0) return true;
+  if (T <= 64 * kWaves)
+    hipLaunchKernelGGL((grad_kernel<1, Op>), dim3((unsigned)(T + 255) / 256), dim3(256), 0, s, op);
+  else
+    hipLaunchKernelGGL((grad_kernel<4, Op>), dim3((unsigned)(T + 1023) / 1024), dim3(256), 0, s, op);
   return launched_ok();
 }
 
@@ -409,8 +500,9 @@ bool backward(const Op& op, hipStream_t s) {
 
 SeqPlan seq_plan(int T, int S) {
   SeqPlan p;
-  const int rounds = (T + kRound - 1) / kRound;
-  p.chunk = kRound * ((rounds + 4095) / 4096 > 0 ? (rounds + 4095) / 4096 : 1);
+  const int most = T <= 2048 ? 16 : kWaves;
+  p.chunk = 64 * std::max(1, (T + 64 * most - 1) / (64 * most));
+  if (p.chunk > 128) p.chunk = (p.chunk + 255) / 256 * 256;
   p.chunks = (T + p.chunk - 1) / p.chunk;
   p.slots = (int64_t)p.chunks + S;
   return p;
