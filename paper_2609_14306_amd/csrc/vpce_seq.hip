@@ -15,7 +15,10 @@ namespace vpce {
 
 namespace {
 
-constexpr int kWaves = 4096;  // wavefronts that fill the chip: four on each of 1024 SIMDs
+// Wavefronts that the tokens are spread over, 64 tokens at a time each: rounds of 64 leave
+// few tokens to the scans, and enough of them hide each other's loads and arithmetic (4.2 M
+// tokens, policy forward: 16384 wavefronts 30.6 us, 4096 with four loads on their way 33.1).
+constexpr int kWaves = 16384;
 
 __device__ __forceinline__ int lane_id() { return threadIdx.x & 63; }
 
@@ -129,8 +132,8 @@ struct Window {
 //
 // The sums of the sequence that a chunk is in stay spread over the lanes as long as it
 // lasts.  64 tokens that hold an end go through a segmented scan, which takes the same
-// time for one end or 63.  J: tokens a lane loads at a time, the next ones on their way.
-template <int J, class Op>
+// time for one end or 63.  The next 64 tokens are on their way meanwhile.
+template <class Op>
 __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
   constexpr int K = Op::K;
   const SeqArgs& q = op.a.q;
@@ -146,59 +149,44 @@ __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
   double acc[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) acc[k] = 0.0;
-  typename Op::Raw raw[J], next[J];
-  auto load = [&](int base) {
-#pragma unroll
-    for (int j = 0; j < J; ++j) op.load(next[j], min(base + 64 * j + lane, t1 - 1));
-  };
-  load(t0);
+  typename Op::Raw raw, next;
+  op.load(next, min(t0 + lane, t1 - 1));
   Window w;
   int s = w.open(q, t0), end = w.end(q, s);  // the sequence that the walk is in, and its end
-  for (int base = t0; base < t1; base += 64 * J) {
+  for (int b = t0; b < t1; b += 64) {
+    const int e = min(b + 64, t1);
+    raw = next;
+    if (e < t1) op.load(next, min(e + lane, t1 - 1));
+    const bool cut = e > end;
+    const int mine = cut ? w.walk(q, b, e - 1) : s;
+    double v[K];
 #pragma unroll
-    for (int j = 0; j < J; ++j) raw[j] = next[j];
-    if (base + 64 * J < t1) load(base + 64 * J);
-    if (min(base + 64 * J, t1) <= end) {
-      if (s >= 0 && s < q.S)
+    for (int k = 0; k < K; ++k) v[k] = 0.0;
+    if (b + lane < e && mine >= 0 && mine < q.S) op.add(v, raw, mine);
+    if (!cut) {
 #pragma unroll
-        for (int j = 0; j < J; ++j)
-          if (base + 64 * j + lane < t1) op.add(acc, raw[j], s);
+      for (int k = 0; k < K; ++k) acc[k] += v[k];
       continue;
     }
-#pragma unroll 1
-    for (int b = base; b < min(base + 64 * J, t1); b += 64) {
-      const int e = min(b + 64, t1);
-      typename Op::Raw r = raw[0];
-      if (J > 1) op.load(r, min(b + lane, t1 - 1));
-      if (e <= end) {
-        if (b + lane < e && s >= 0 && s < q.S) op.add(acc, r, s);
-        continue;
-      }
-      wave_sum(acc);
-      const int mine = w.walk(q, b, e - 1);
-      double v[K];
+    wave_sum(acc);
+    const int up = __shfl_up(mine, 1), down = __shfl_down(mine, 1);
+    const bool head = mine != (lane ? up : s);
+    if (lane == 0) {
+      if (head)
+        put(s, acc);
+      else
 #pragma unroll
-      for (int k = 0; k < K; ++k) v[k] = 0.0;
-      if (b + lane < e && mine >= 0 && mine < q.S) op.add(v, r, mine);
-      const int up = __shfl_up(mine, 1), down = __shfl_down(mine, 1);
-      const bool head = mine != (lane ? up : s);
-      if (lane == 0) {
-        if (head)
-          put(s, acc);
-        else
+        for (int k = 0; k < K; ++k) v[k] += acc[k];
+    }
+    segmented_scan(v, (int)head);
+    if (lane < 63 && down != mine) put(mine, v);
+    // the last lane's sequence goes on
+    s = __builtin_amdgcn_readlane(mine, 63);
+    end = w.end(q, s);
 #pragma unroll
-          for (int k = 0; k < K; ++k) v[k] += acc[k];
-      }
-      segmented_scan(v, (int)head);
-      if (lane < 63 && down != mine) put(mine, v);
-      // the last lane's sequence goes on
-      s = __builtin_amdgcn_readlane(mine, 63);
-      end = w.end(q, s);
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const double x = lane_read(v[k], 63);
-        acc[k] = lane ? 0.0 : x;
-      }
+    for (int k = 0; k < K; ++k) {
+      const double x = lane_read(v[k], 63);
+      acc[k] = lane ? 0.0 : x;
     }
   }
   wave_sum(acc);
@@ -215,16 +203,71 @@ __device__ __forceinline__ bool sequence_sums(const SeqArgs& q, int s, double (&
   for (int k = 0; k < K; ++k) v[k] = 0.0;
   if (good && a < b) {
     const int last = (b - 1) / q.chunk;
-#pragma unroll 2
+#pragma unroll 8
     for (int c = a / q.chunk + (int)(threadIdx.x % LANES); c <= last; c += LANES)
 #pragma unroll
       for (int k = 0; k < K; ++k) v[k] += q.part[(int64_t)(c + s) * K + k];
   }
+  if constexpr (LANES >= 64) {
+    wave_sum(v);
+  } else {
 #pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1)
+    for (int o = LANES / 2; o > 0; o >>= 1)
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o);
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o);
+  }
+  if constexpr (LANES > 64) {  // a workgroup
+    __shared__ double side[LANES / 64][K];
+    __syncthreads();  // (of the sequence before)
+    if (lane_id() == 0)
+#pragma unroll
+      for (int k = 0; k < K; ++k) side[threadIdx.x >> 6][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      v[k] = side[0][k];
+#pragma unroll
+      for (int w = 1; w < LANES / 64; ++w) v[k] += side[w][k];
+    }
+  }
   return good;
+}
+
+// e^x and e^x - 1: x = n ln 2 + r with |r| <= 0.3466, p = e^r - 1 by its series up to
+// r^13 / 13! (the next term is below 2^-59 r), e^x = 2^n (1 + p).  e^x - 1 is p itself for
+// n = 0 and loses at most two bits to the difference otherwise.  Half the instructions of
+// the library's exp and expm1, which also carry their answers to the last bit.
+__device__ __forceinline__ void exp_both(double x, double& e, double& em1) {
+  const double y = fmin(fmax(x, -1100.0), 1100.0);
+  const double n = rint(y * 1.4426950408889634);
+  double r = fma(n, -0.6931471805599453, y);
+  r = fma(n, -2.3190468138462996e-17, r);
+  double p = 1.0 / 6227020800.0;
+  p = fma(p, r, 1.0 / 479001600.0);
+  p = fma(p, r, 1.0 / 39916800.0);
+  p = fma(p, r, 1.0 / 3628800.0);
+  p = fma(p, r, 1.0 / 362880.0);
+  p = fma(p, r, 1.0 / 40320.0);
+  p = fma(p, r, 1.0 / 5040.0);
+  p = fma(p, r, 1.0 / 720.0);
+  p = fma(p, r, 1.0 / 120.0);
+  p = fma(p, r, 1.0 / 24.0);
+  p = fma(p, r, 1.0 / 6.0);
+  p = fma(p, r, 0.5);
+  p = fma(p * r, r, r);
+  e = ldexp(1.0 + p, (int)n);
+  em1 = n == 0.0 ? p : e - 1.0;
+  if (!(x == x)) e = em1 = x;
+}
+
+// log(1 + e) for 0 <= e <= 1: 2 atanh(u), u = e / (2 + e) <= 1/3, by its series up to
+// u^29 / 29 (the next term is below 2^-51 u).
+__device__ __forceinline__ double log_1_plus(double e) {
+  const double u = e / (2.0 + e), w = u * u;
+  double p = 1.0 / 29.0;
+#pragma unroll
+  for (int k = 27; k >= 1; k -= 2) p = fma(p, w, 1.0 / k);
+  return 2.0 * u * p;
 }
 
 // A preference pair from its two log ratio sums and token counts.
@@ -239,8 +282,10 @@ __device__ void finish_pair(const PrefArgs& a, int pair, const double (&sum)[2],
   const double z = reward[0] - reward[1] - a.margin;
   double loss, slope;
   if (a.kind == VP_PREF_LOGISTIC) {
-    const double e = exp(-fabs(z)), l = log1p(e);
-    const double pos = 1.0 / (1.0 + e), neg = e / (1.0 + e);  // sigmoid of |z| and of -|z|
+    double e, unused;
+    exp_both(-fabs(z), e, unused);
+    const double l = log_1_plus(e);
+    const double pos = 1.0 / (1.0 + e), neg = e * pos;  // sigmoid of |z| and of -|z|
     loss = (1.0 - a.smoothing) * (l + fmax(-z, 0.0));
     if (a.smoothing > 0.0) loss += a.smoothing * (l + fmax(z, 0.0));  // (an infinite z has weight 0 here)
     slope = a.smoothing * (z >= 0.0 ? pos : neg) - (1.0 - a.smoothing) * (z >= 0.0 ? neg : pos);
@@ -289,33 +334,6 @@ struct PrefOp {
     if (threadIdx.x % LANES == 0) finish_pair(a, pair, sum, n, good);
   }
 };
-
-// e^x and e^x - 1: x = n ln 2 + r with |r| <= 0.3466, p = e^r - 1 by its series up to
-// r^13 / 13! (the next term is below 2^-59 r), e^x = 2^n (1 + p).  e^x - 1 is p itself for
-// n = 0 and loses at most two bits to the difference otherwise.  Half the instructions of
-// the library's exp and expm1, which also carry their answers to the last bit.
-__device__ __forceinline__ void exp_both(double x, double& e, double& em1) {
-  const double y = fmin(fmax(x, -1100.0), 1100.0);
-  const double n = rint(y * 1.4426950408889634);
-  double r = fma(n, -0.6931471805599453, y);
-  r = fma(n, -2.3190468138462996e-17, r);
-  double p = 1.0 / 6227020800.0;
-  p = fma(p, r, 1.0 / 479001600.0);
-  p = fma(p, r, 1.0 / 39916800.0);
-  p = fma(p, r, 1.0 / 3628800.0);
-  p = fma(p, r, 1.0 / 362880.0);
-  p = fma(p, r, 1.0 / 40320.0);
-  p = fma(p, r, 1.0 / 5040.0);
-  p = fma(p, r, 1.0 / 720.0);
-  p = fma(p, r, 1.0 / 120.0);
-  p = fma(p, r, 1.0 / 24.0);
-  p = fma(p, r, 1.0 / 6.0);
-  p = fma(p, r, 0.5);
-  p = fma(p * r, r, r);
-  e = ldexp(1.0 + p, (int)n);
-  em1 = n == 0.0 ? p : e - 1.0;
-  if (!(x == x)) e = em1 = x;
-}
 
 // The policy loss of one token and its slope in loss_t.
 struct PolicyToken {
@@ -389,10 +407,10 @@ struct PolicyOp {
   }
 };
 
-template <int J, class Op, class Args>
+template <class Op, class Args>
 __global__ void __launch_bounds__(256) chunk_kernel(Args args) {
   const Op op{args};
-  chunk_sums<J>(op, __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  chunk_sums(op, __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)));
 }
 template <class Op, class Args, int LANES>
 __global__ void __launch_bounds__(256) finish_kernel(Args args) {
@@ -404,13 +422,16 @@ __global__ void __launch_bounds__(256) finish_kernel(Args args) {
 template <class Op, class Args>
 __global__ void __launch_bounds__(1024) small_kernel(Args args) {
   const Op op{args};
-  chunk_sums<1>(op, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  chunk_sums(op, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
   __syncthreads();
   for (int unit = threadIdx.x; unit < args.q.S / Op::PER_UNIT; unit += 1024) op.template finish<1>(unit);
 }
 
-// Gradients: J tokens a lane.
+// Gradients: J tokens a lane, one where that does not fill the chip.  The more a token
+// brings with it, the fewer: 4 M tokens, J = 1 / 2 / 4: preference 14.9 / 11.4 / 9.9 us, policy
+// 27.5 / 25.2 / 27.2 us; 32768 tokens, policy 3.4 / 4.6 / 6.4 us.
 struct PrefGrad {
+  static constexpr int J = 4;
   SeqArgs q;
   const float* coef;
   const float* grad_pair;
@@ -422,6 +443,7 @@ struct PrefGrad {
   __device__ __forceinline__ float grad(const Raw&, int s) const { return grad_pair[s >> 1] * coef[s]; }
 };
 struct PolicyGrad {
+  static constexpr int J = 2;
   PolicyArgs a;
   SeqArgs q;
   float* grad_loss;
@@ -463,6 +485,12 @@ __global__ void __launch_bounds__(256) grad_kernel(Op op) {
 
 bool launched_ok() { return hipGetLastError() == hipSuccess; }
 
+template <class Op, class Args, int LANES>
+void launch_finish(const Args& a, int units, hipStream_t s) {
+  constexpr int PER = 256 / LANES;
+  hipLaunchKernelGGL((finish_kernel<Op, Args, LANES>), dim3((unsigned)(units + PER - 1) / PER), dim3(256), 0, s, a);
+}
+
 template <class Op, class Args>
 bool forward(const Args& a, hipStream_t s) {
   const SeqArgs& q = a.q;
@@ -473,26 +501,31 @@ bool forward(const Args& a, hipStream_t s) {
     return launched_ok();
   }
   const dim3 grid((unsigned)(p.chunks + 3) / 4);
-  if (p.chunk <= 128)
-    hipLaunchKernelGGL((chunk_kernel<1, Op, Args>), grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((chunk_kernel<4, Op, Args>), grid, dim3(256), 0, s, a);
+  hipLaunchKernelGGL((chunk_kernel<Op, Args>), grid, dim3(256), 0, s, a);
   if (!launched_ok()) return false;
   const int units = q.S / Op::PER_UNIT;
-  if (units <= 16384)
-    hipLaunchKernelGGL((finish_kernel<Op, Args, 64>), dim3((unsigned)(units + 3) / 4), dim3(256), 0, s, a);
+  if (p.chunks >= 512 * (int64_t)units)
+    launch_finish<Op, Args, 256>(a, units, s);
+  else if (units <= 16384)
+    launch_finish<Op, Args, 64>(a, units, s);
   else
-    hipLaunchKernelGGL((finish_kernel<Op, Args, 8>), dim3((unsigned)(units + 31) / 32), dim3(256), 0, s, a);
+    launch_finish<Op, Args, 8>(a, units, s);
   return launched_ok();
 }
+template <int J, class Op>
+void launch_grad(const Op& op, hipStream_t s) {
+  constexpr int PER = 256 * J;
+  hipLaunchKernelGGL((grad_kernel<J, Op>), dim3((unsigned)(op.q.T + PER - 1) / PER), dim3(256), 0, s, op);
+}
+
 template <class Op>
 bool backward(const Op& op, hipStream_t s) {
   const int T = op.q.T;
   if (T == 0) return true;
   if (T <= 64 * kWaves)
-    hipLaunchKernelGGL((grad_kernel<1, Op>), dim3((unsigned)(T + 255) / 256), dim3(256), 0, s, op);
+    launch_grad<1>(op, s);
   else
-    hipLaunchKernelGGL((grad_kernel<4, Op>), dim3((unsigned)(T + 1023) / 1024), dim3(256), 0, s, op);
+    launch_grad<Op::J>(op, s);
   return launched_ok();
 }
 
@@ -502,7 +535,6 @@ SeqPlan seq_plan(int T, int S) {
   SeqPlan p;
   const int most = T <= 2048 ? 16 : kWaves;
   p.chunk = 64 * std::max(1, (T + 64 * most - 1) / (64 * most));
-  if (p.chunk > 128) p.chunk = (p.chunk + 255) / 256 * 256;
   p.chunks = (T + p.chunk - 1) / p.chunk;
   p.slots = (int64_t)p.chunks + S;
   return p;
