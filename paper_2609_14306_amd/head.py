@@ -8,7 +8,7 @@ runs on the device of its tensors, on that device's current stream unless `strea
 from __future__ import annotations
 
 import ctypes
-from typing import Optional
+from functools import cached_property
 
 from . import (VP_ACCUMULATE_DW, VP_ADV_PER_TOKEN, VP_ERR_WORKSPACE, VP_NORM_RMS, VP_PREF_LOGISTIC,
                VP_PREF_SQUARED, VP_SEQ_MEAN, _check, _dtype_code, _need, _need_ws, _same_device, _torch_dtype,
@@ -24,6 +24,25 @@ class Norm:
         self.ref = ctypes.byref(self.c)
         self.T, self.d, self.rms = int(T), int(d), bool(rms)
 
+    @cached_property
+    def forward_spec(self):
+        import torch
+        f, x = torch.float32, _torch_dtype(self.c.dtype)
+        Td, d, T = (self.T, self.d), (self.d,), (self.T,)
+        return _spec(f"X gamma beta? Y {self._mean} rstd", (x, x, x, x, f, f), (Td, d, d, Td, T, T))
+
+    @cached_property
+    def backward_spec(self):
+        import torch
+        f, x = torch.float32, _torch_dtype(self.c.dtype)
+        Td, d, T = (self.T, self.d), (self.d,), (self.T,)
+        return _spec(f"X gamma {self._mean} rstd dY dX dgamma dbeta?", (x, x, f, f, f, f, f, f),
+                     (Td, d, T, T, Td, Td, d, d))
+
+    @property
+    def _mean(self):
+        return "mean?" if self.rms else "mean"
+
 
 class Sequences:
     """A ``vp_sequences``: T packed tokens in S sequences; `mean` weights each sequence's sum by
@@ -33,6 +52,37 @@ class Sequences:
         self.c = vp_sequences(T=int(T), S=int(S), ignore_index=int(ignore_index), flags=VP_SEQ_MEAN if mean else 0)
         self.ref = ctypes.byref(self.c)
         self.T, self.S, self.mean = int(T), int(S), bool(mean)
+
+    def _spec(self, names, dtypes, shapes):
+        import torch
+        return _spec("start targets " + names, (torch.int32, torch.int64) + dtypes,
+                     ((self.S + 1,), (self.T,)) + shapes)
+
+    @cached_property
+    def pref_forward_spec(self):
+        import torch
+        T, S, N = (self.T,), (self.S,), (self.S // 2,)
+        return self._spec("loss ref_loss? pair_loss reward coef", (torch.float32,) * 5, (T, T, N, S, S))
+
+    @cached_property
+    def pref_backward_spec(self):
+        import torch
+        return self._spec("coef grad_pair grad_loss", (torch.float32,) * 3, ((self.S,), (self.S // 2,), (self.T,)))
+
+    # by whether the advantage is one value per token
+    @cached_property
+    def policy_forward_spec(self):
+        import torch
+        f, i, T, S = torch.float32, torch.int32, (self.T,), (self.S,)
+        return [self._spec("loss old_loss? ref_loss? advantage seq_loss seq_kl clipped tokens",
+                           (f, f, f, f, f, f, i, i), (T, T, T, adv, S, S, S, S)) for adv in (S, T)]
+
+    @cached_property
+    def policy_backward_spec(self):
+        import torch
+        f, T, S = torch.float32, (self.T,), (self.S,)
+        return [self._spec(f"loss old_loss? ref_loss? advantage {'tokens' if self.mean else 'tokens?'} grad_seq grad_loss",
+                           (f, f, f, f, torch.int32, f, f), (T, T, T, adv, S, S, T)) for adv in (S, T)]
 
 
 class Preference:
@@ -66,44 +116,61 @@ class HeadNorm:
 
 
 # ---------------------------------------------------------------------------
-def _call(fn: str, head, named, ws, need, stream) -> None:
-    """Checks `named` = (name, tensor, dtype, shape) and calls ``fn(*head, *pointers, stream)``.
-    A name that ends in "?" may be None.  ws: the workspace of `need()` bytes, between the
-    pointers and the stream; False for calls without one."""
+# A call's tensors, in the order of the C entry: names (one that ends in "?" may be None), dtypes
+# and shapes.  The problems build each once, so that a call's checks are one pass of about 0.25 us
+# a tensor; what a tensor is, and where, is looked up on every call.
+def _spec(names, dtypes, shapes):
+    return tuple((n, n[-1] == "?", dt, tuple(sh)) for n, dt, sh in zip(names.split(), dtypes, shapes))
+
+
+def _raw_stream(dev: int) -> int:
     import torch
-    args, dev, alike = list(head), -1, True
-    for name, t, dtype, shape in named:
-        if t is None and name[-1] == "?":
-            args.append(None)
-            continue
-        try:
-            good = t.dtype == dtype and t.shape == shape and t.is_contiguous()
-        except AttributeError:  # not a tensor
-            good = False
-        if not good:
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 1 us less than a Stream object
+    return int(get(dev) if get is not None else torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _refuse(spec, tensors, ws, need) -> None:
+    for (name, may, dtype, shape), t in zip(spec, tensors):
+        if not (may and t is None):
             _need(t, name.rstrip("?"), dtype, shape)
-        at = t.get_device()
-        alike &= at >= 0 and (dev < 0 or at == dev)
-        dev = at if dev < 0 else dev
-        args.append(t.data_ptr())
     if ws is not False:
-        if not isinstance(ws, torch.Tensor) or not ws.is_contiguous():
-            _need_ws(ws, 0)
-        args += [ws.data_ptr(), ws.numel() * ws.element_size()]
-        alike &= ws.get_device() == dev
-    if not alike:
-        if ws is not False:
-            _need_ws(ws, need())
-        _same_device([(n, t) for n, t, _, _ in named] + ([] if ws is False else [("ws", ws)]))
-    lib = load_library()
-    args.append(int(stream) if stream is not None else int(torch.cuda.current_stream(dev).cuda_stream))
+        _need_ws(ws, need())
+    _same_device([(n[0].rstrip("?"), t) for n, t in zip(spec, tensors)] + ([] if ws is False else [("ws", ws)]))
+
+
+def _call(fn: str, head, spec, tensors, stream, ws=False, need=None) -> None:
+    """Checks `tensors` against `spec` and calls ``fn(*head, *pointers, stream)``.  ws: the
+    workspace of `need()` bytes, between the pointers and the stream; False for calls without."""
+    import torch
+    args = list(head)
+    try:
+        dev = tensors[0].get_device()
+        good = dev >= 0
+        for (_, may, dtype, shape), t in zip(spec, tensors):
+            if may and t is None:
+                args.append(None)
+            elif t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+                args.append(t.data_ptr())
+            else:
+                good = False
+                break
+        if good and ws is not False:
+            good = ws.get_device() == dev and ws.is_contiguous()
+            args += (ws.data_ptr(), ws.numel() * ws.element_size())
+    except AttributeError:  # not a tensor
+        good = False
+    if not good:
+        _refuse(spec, tensors, ws, need)
+        raise ValueError(f"{fn}: unsupported tensors")
+    args.append(_raw_stream(dev) if stream is None else int(stream))
+    call = getattr(load_library(), fn)
     if torch.cuda.current_device() == dev:
-        st = getattr(lib, fn)(*args)
+        st = call(*args)
     else:
         with torch.cuda.device(dev):
-            st = getattr(lib, fn)(*args)
+            st = call(*args)
     if st == VP_ERR_WORKSPACE:
-        _need_ws(ws, need())
+        _refuse(spec, tensors, ws, need)
     _check(st, fn)
 
 
@@ -116,21 +183,13 @@ def vp_norm_workspace_size(norm: Norm) -> int:
 
 def vp_norm_forward(norm: Norm, X, gamma, beta, Y, mean, rstd, stream=None) -> None:
     """Y and the row statistics of X.  beta may be None, and mean in the RMS form."""
-    import torch
-    f32, dt, Td, d, T = torch.float32, _torch_dtype(norm.c.dtype), (norm.T, norm.d), (norm.d,), (norm.T,)
-    _call("vp_norm_forward", (norm.ref,),
-          (("X", X, dt, Td), ("gamma", gamma, dt, d), ("beta?", beta, dt, d), ("Y", Y, dt, Td),
-           ("mean?" if norm.rms else "mean", mean, f32, T), ("rstd", rstd, f32, T)), False, None, stream)
+    _call("vp_norm_forward", (norm.ref,), norm.forward_spec, (X, gamma, beta, Y, mean, rstd), stream)
 
 
 def vp_norm_backward(norm: Norm, X, gamma, mean, rstd, dY, dX, dgamma, dbeta, ws, stream=None) -> None:
     """dX (which may be dY), dgamma and dbeta (None: not computed)."""
-    import torch
-    f32, dt, Td, d, T = torch.float32, _torch_dtype(norm.c.dtype), (norm.T, norm.d), (norm.d,), (norm.T,)
-    _call("vp_norm_backward", (norm.ref,),
-          (("X", X, dt, Td), ("gamma", gamma, dt, d), ("mean?" if norm.rms else "mean", mean, f32, T),
-           ("rstd", rstd, f32, T), ("dY", dY, f32, Td), ("dX", dX, f32, Td), ("dgamma", dgamma, f32, d),
-           ("dbeta?", dbeta, f32, d)), ws, lambda: vp_norm_workspace_size(norm), stream)
+    _call("vp_norm_backward", (norm.ref,), norm.backward_spec, (X, gamma, mean, rstd, dY, dX, dgamma, dbeta), stream,
+          ws, lambda: vp_norm_workspace_size(norm))
 
 
 def vp_seq_workspace_size(seq: Sequences) -> int:
@@ -143,54 +202,29 @@ def vp_seq_workspace_size(seq: Sequences) -> int:
 def vp_pref_forward(seq: Sequences, pref: Preference, start, targets, loss, ref_loss, pair_loss, reward, coef, ws,
                     stream=None) -> None:
     """pair_loss [S/2], reward [S] and coef [S] of S/2 pairs.  ref_loss may be None."""
-    import torch
-    f32, T, S = torch.float32, (seq.T,), (seq.S,)
-    _call("vp_pref_forward", (seq.ref, pref.ref),
-          (("start", start, torch.int32, (seq.S + 1,)), ("targets", targets, torch.int64, T), ("loss", loss, f32, T),
-           ("ref_loss?", ref_loss, f32, T), ("pair_loss", pair_loss, f32, (seq.S // 2,)), ("reward", reward, f32, S),
-           ("coef", coef, f32, S)), ws, lambda: vp_seq_workspace_size(seq), stream)
+    _call("vp_pref_forward", (seq.ref, pref.ref), seq.pref_forward_spec,
+          (start, targets, loss, ref_loss, pair_loss, reward, coef), stream, ws, lambda: vp_seq_workspace_size(seq))
 
 
 def vp_pref_backward(seq: Sequences, start, targets, coef, grad_pair, grad_loss, stream=None) -> None:
     """grad_loss [T] from the forward's coef and the upstream gradient grad_pair [S/2]."""
-    import torch
-    f32, T = torch.float32, (seq.T,)
-    _call("vp_pref_backward", (seq.ref,),
-          (("start", start, torch.int32, (seq.S + 1,)), ("targets", targets, torch.int64, T),
-           ("coef", coef, f32, (seq.S,)), ("grad_pair", grad_pair, f32, (seq.S // 2,)),
-           ("grad_loss", grad_loss, f32, T)), False, None, stream)
-
-
-def _policy_inputs(seq: Sequences, policy: Policy, start, targets, loss, old_loss, ref_loss, advantage):
-    import torch
-    f32, T = torch.float32, (seq.T,)
-    return (("start", start, torch.int32, (seq.S + 1,)), ("targets", targets, torch.int64, T), ("loss", loss, f32, T),
-            ("old_loss?", old_loss, f32, T), ("ref_loss?", ref_loss, f32, T),
-            ("advantage", advantage, f32, T if policy.per_token else (seq.S,)))
+    _call("vp_pref_backward", (seq.ref,), seq.pref_backward_spec, (start, targets, coef, grad_pair, grad_loss), stream)
 
 
 def vp_policy_forward(seq: Sequences, policy: Policy, start, targets, loss, old_loss, ref_loss, advantage, seq_loss,
                       seq_kl, clipped, tokens, ws, stream=None) -> None:
     """seq_loss, seq_kl (float32) and clipped, tokens (int32) [S].  old_loss and ref_loss may be None."""
-    import torch
-    S = (seq.S,)
-    _call("vp_policy_forward", (seq.ref, policy.ref),
-          _policy_inputs(seq, policy, start, targets, loss, old_loss, ref_loss, advantage) +
-          (("seq_loss", seq_loss, torch.float32, S), ("seq_kl", seq_kl, torch.float32, S),
-           ("clipped", clipped, torch.int32, S), ("tokens", tokens, torch.int32, S)),
-          ws, lambda: vp_seq_workspace_size(seq), stream)
+    _call("vp_policy_forward", (seq.ref, policy.ref), seq.policy_forward_spec[policy.per_token],
+          (start, targets, loss, old_loss, ref_loss, advantage, seq_loss, seq_kl, clipped, tokens), stream, ws,
+          lambda: vp_seq_workspace_size(seq))
 
 
 def vp_policy_backward(seq: Sequences, policy: Policy, start, targets, loss, old_loss, ref_loss, advantage, tokens,
                        grad_seq, grad_loss, stream=None) -> None:
     """grad_loss [T] from the upstream gradient grad_seq [S]; tokens (from the forward) may be None
     without the mean."""
-    import torch
-    _call("vp_policy_backward", (seq.ref, policy.ref),
-          _policy_inputs(seq, policy, start, targets, loss, old_loss, ref_loss, advantage) +
-          (("tokens" if seq.mean else "tokens?", tokens, torch.int32, (seq.S,)),
-           ("grad_seq", grad_seq, torch.float32, (seq.S,)), ("grad_loss", grad_loss, torch.float32, (seq.T,))),
-          False, None, stream)
+    _call("vp_policy_backward", (seq.ref, policy.ref), seq.policy_backward_spec[policy.per_token],
+          (start, targets, loss, old_loss, ref_loss, advantage, tokens, grad_seq, grad_loss), stream)
 
 
 # ---------------------------------------------------------------------------
