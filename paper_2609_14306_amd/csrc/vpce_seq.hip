@@ -125,6 +125,9 @@ struct Window {
   }
 };
 
+// A sequence that exists in place of -1 and S, whose values are read and not used.
+__device__ __forceinline__ int clip(int s, const SeqArgs& q) { return min(max(s, 0), max(q.S - 1, 0)); }
+
 // Partial sums.  The tokens are cut into chunks of q.chunk, a wavefront each, and chunk c
 // leaves its part of sequence s in slot c + s: walking the tokens, every step to another
 // chunk or sequence makes c + s larger, so no two parts share a slot, and chunks + S slots
@@ -153,6 +156,7 @@ __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
   op.load(next, min(t0 + lane, t1 - 1));
   Window w;
   int s = w.open(q, t0), end = w.end(q, s);  // the sequence that the walk is in, and its end
+  typename Op::Seq here = op.open(clip(s, q));
   for (int b = t0; b < t1; b += 64) {
     const int e = min(b + 64, t1);
     raw = next;
@@ -162,7 +166,12 @@ __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
     double v[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = 0.0;
-    if (b + lane < e && mine >= 0 && mine < q.S) op.add(v, raw, mine);
+    typename Op::Seq seq = here;
+    if (cut) {
+      seq = op.open(clip(mine, q));
+      seq.wait();  // here, where there is something to wait for
+    }
+    if (b + lane < e && mine >= 0 && mine < q.S) op.add(v, raw, seq);
     if (!cut) {
 #pragma unroll
       for (int k = 0; k < K; ++k) acc[k] += v[k];
@@ -183,6 +192,7 @@ __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
     // the last lane's sequence goes on
     s = __builtin_amdgcn_readlane(mine, 63);
     end = w.end(q, s);
+    here = op.open(clip(s, q));
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const double x = lane_read(v[k], 63);
@@ -234,7 +244,7 @@ __device__ __forceinline__ bool sequence_sums(const SeqArgs& q, int s, double (&
 }
 
 // e^x and e^x - 1: x = n ln 2 + r with |r| <= 0.3466, p = e^r - 1 by its series up to
-// r^13 / 13! (the next term is below 2^-59 r), e^x = 2^n (1 + p).  e^x - 1 is p itself for
+// r^11 / 11! (what is left out is below 2^-45 r), e^x = 2^n (1 + p).  e^x - 1 is p itself for
 // n = 0 and loses at most two bits to the difference otherwise.  Half the instructions of
 // the library's exp and expm1, which also carry their answers to the last bit.
 __device__ __forceinline__ void exp_both(double x, double& e, double& em1) {
@@ -242,9 +252,7 @@ __device__ __forceinline__ void exp_both(double x, double& e, double& em1) {
   const double n = rint(y * 1.4426950408889634);
   double r = fma(n, -0.6931471805599453, y);
   r = fma(n, -2.3190468138462996e-17, r);
-  double p = 1.0 / 6227020800.0;
-  p = fma(p, r, 1.0 / 479001600.0);
-  p = fma(p, r, 1.0 / 39916800.0);
+  double p = 1.0 / 39916800.0;
   p = fma(p, r, 1.0 / 3628800.0);
   p = fma(p, r, 1.0 / 362880.0);
   p = fma(p, r, 1.0 / 40320.0);
@@ -315,7 +323,11 @@ struct PrefOp {
     r.loss = a.loss[t];
     r.ref = a.ref ? a.ref[t] : 0.f;
   }
-  __device__ __forceinline__ void add(double (&v)[K], const Raw& r, int) const {
+  struct Seq {
+    __device__ void wait() {}
+  };
+  __device__ __forceinline__ Seq open(int) const { return {}; }
+  __device__ __forceinline__ void add(double (&v)[K], const Raw& r, const Seq&) const {
     if (r.target == a.q.ignore_index) return;
     v[0] += (double)r.ref - (double)r.loss;
     v[1] += 1.0;
@@ -385,9 +397,14 @@ struct PolicyOp {
   using Raw = PolicyRaw;
   const PolicyArgs& a;
   __device__ __forceinline__ void load(Raw& r, int t) const { load_token(a, r, t); }
-  __device__ __forceinline__ void add(double (&v)[K], const Raw& r, int s) const {
+  struct Seq {
+    float adv;
+    __device__ __forceinline__ void wait() { asm volatile("" : "+v"(adv)); }
+  };
+  __device__ __forceinline__ Seq open(int s) const { return {a.per_token ? 0.f : a.adv[s]}; }
+  __device__ __forceinline__ void add(double (&v)[K], const Raw& r, const Seq& seq) const {
     if (r.target == a.q.ignore_index) return;
-    const PolicyToken p = policy_token(a, r, (double)(a.per_token ? r.adv : a.adv[s]));
+    const PolicyToken p = policy_token(a, r, (double)(a.per_token ? r.adv : seq.adv));
     v[0] += p.loss;
     v[1] += p.kl;
     v[2] += p.clipped ? kClip + 1.0 : 1.0;
@@ -440,7 +457,11 @@ struct PrefGrad {
     int64_t target;
   };
   __device__ __forceinline__ void load(Raw& r, int t) const { r.target = q.targets[t]; }
-  __device__ __forceinline__ float grad(const Raw&, int s) const { return grad_pair[s >> 1] * coef[s]; }
+  struct Seq {
+    float grad;
+  };
+  __device__ __forceinline__ Seq open(int s) const { return {grad_pair[s >> 1] * coef[s]}; }
+  __device__ __forceinline__ float grad(const Raw&, const Seq& s) const { return s.grad; }
 };
 struct PolicyGrad {
   static constexpr int J = 2;
@@ -449,10 +470,16 @@ struct PolicyGrad {
   float* grad_loss;
   using Raw = PolicyRaw;
   __device__ __forceinline__ void load(Raw& r, int t) const { load_token(a, r, t); }
-  __device__ __forceinline__ float grad(const Raw& r, int s) const {
-    const double c = q.mean ? 1.0 / (double)max(a.tokens[s], 1) : 1.0;
-    return (float)((double)a.grad_seq[s] * c *
-                   policy_token(a, r, (double)(a.per_token ? r.adv : a.adv[s])).slope);
+  struct Seq {
+    float adv;
+    double weight;
+  };
+  __device__ __forceinline__ Seq open(int s) const {
+    return {a.per_token ? 0.f : a.adv[s],
+            (double)a.grad_seq[s] * (q.mean ? 1.0 / (double)max(a.tokens[s], 1) : 1.0)};
+  }
+  __device__ __forceinline__ float grad(const Raw& r, const Seq& s) const {
+    return (float)(s.weight * policy_token(a, r, (double)(a.per_token ? r.adv : s.adv)).slope);
   }
 };
 template <int J, class Op>
@@ -466,19 +493,29 @@ __global__ void __launch_bounds__(256) grad_kernel(Op op) {
   for (int j = 0; j < J; ++j) op.load(raw[j], min(base + 64 * j + lane, q.T - 1));
   Window w;
   int s = w.open(q, base), end = w.end(q, s);
+  if (q.S == 0) {
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      if (base + 64 * j + lane < q.T) op.grad_loss[base + 64 * j + lane] = 0.f;
+    return;
+  }
+  typename Op::Seq here = op.open(clip(s, q));
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int b = base + 64 * j, e = min(b + 64, q.T);
     if (b >= q.T) break;
     int mine = s;
+    typename Op::Seq seq = here;
     if (e > end) {
       mine = w.walk(q, b, e - 1);
+      seq = op.open(clip(mine, q));
       s = __builtin_amdgcn_readlane(mine, 63);
       end = w.end(q, s);
+      if (j + 1 < J) here = op.open(clip(s, q));
     }
     if (b + lane < e) {
       const bool counts = mine >= 0 && mine < q.S && raw[j].target != q.ignore_index;
-      op.grad_loss[b + lane] = counts ? op.grad(raw[j], mine) : 0.f;
+      op.grad_loss[b + lane] = counts ? op.grad(raw[j], seq) : 0.f;
     }
   }
 }
