@@ -265,7 +265,8 @@ vp_status vp_norm_backward(const vp_norm* norm, const void* X, const void* gamma
  * 0..T; a sequence may be empty; tokens before start[0] or from start[S] on belong to
  * none).  A token counts if it belongs to a sequence and targets[t] != ignore_index:
  * what any other token's entry of a per-token array holds is not used (it may be NaN),
- * and its gradient is 0.  With n_s the counting tokens of sequence s, a sum over it is
+ * and its gradient is 0.  A counting token whose loss is NaN (an out-of-range target)
+ * makes its sequence's results NaN, and no other's.  With n_s the counting tokens of sequence s, a sum over it is
  * weighted by c_s = 1, or with VP_SEQ_MEAN by c_s = 1 / n_s (0 where n_s == 0).
  * Sums are float64, results are rounded once to float32.
  *

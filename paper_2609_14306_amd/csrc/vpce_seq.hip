@@ -533,14 +533,14 @@ bool forward(const Args& a, hipStream_t s) {
   const SeqArgs& q = a.q;
   if (q.S == 0) return true;
   const SeqPlan p = seq_plan(q.T, q.S);
-  if (p.chunks <= 16) {
+  const int units = q.S / Op::PER_UNIT;
+  if (p.chunks <= 16 && units <= 2048) {  // (a workgroup's threads take two units at most)
     hipLaunchKernelGGL((small_kernel<Op, Args>), dim3(1), dim3(1024), 0, s, a);
     return launched_ok();
   }
   const dim3 grid((unsigned)(p.chunks + 3) / 4);
   hipLaunchKernelGGL((chunk_kernel<Op, Args>), grid, dim3(256), 0, s, a);
   if (!launched_ok()) return false;
-  const int units = q.S / Op::PER_UNIT;
   if (p.chunks >= 512 * (int64_t)units)
     launch_finish<Op, Args, 256>(a, units, s);
   else if (units <= 16384)

@@ -159,6 +159,43 @@ def test_policy(layout, old, ref, per_token, kl_coef, mean):
     assert bool((back.cpu()[m["mask"]] == 0).all())
 
 
+@pytest.mark.parametrize("S, T", [(35000, 200003), (40000, 1500), (2 ** 22, 70000)])
+def test_many_sequences(S, T):
+    """More sequences than wavefronts, and many more sequences than tokens; sums by sequence from
+    the plain form of each token."""
+    g = torch.Generator().manual_seed(S)
+    start = torch.cat([torch.zeros(1, dtype=torch.int64), torch.randint(0, T + 1, (S - 1,), generator=g).sort().values,
+                       torch.tensor([T])])
+    loss, old, ref = [(3 * torch.rand(T, generator=g)) for _ in range(3)]
+    targets = torch.where(torch.rand(T, generator=g) < 0.3, IGNORE, 5)
+    adv, up = torch.randn(S, generator=g), torch.rand(S, generator=g)
+    seq = torch.searchsorted(start, torch.arange(T), right=True) - 1
+    keep = targets != IGNORE
+    l, kl, clipped, slope = hp.policy_tokens(loss.double(), old.double(), ref.double(), adv.double()[seq], 0.2, 0.2, 0.1)
+
+    def total(v):
+        return torch.zeros(S, dtype=torch.float64).index_add_(0, seq[keep], v.double()[keep])
+
+    dev = [v.cuda() for v in (loss, targets, start.int())]
+    pol, more = vp.Policy(kl_coef=0.1), dict(old_loss=old.cuda(), ref_loss=ref.cuda())
+    got = vp.policy_forward(*dev, pol, adv.cuda(), **more)
+    # at most 2^12 tokens a sequence, each below e^3 |A| + 0.1 e^3
+    _close(got[0], total(l), 2.0 ** -45 * total(21 * adv.double()[seq].abs() + 3), "seq_loss")
+    _close(got[1], total(kl), 2.0 ** -45 * total(torch.full((T,), 21.0)), "seq_kl")
+    assert torch.equal(got[2].cpu(), total(clipped).int()) and torch.equal(got[3].cpu(), total(keep).int())
+    back = vp.policy_backward(*dev, pol, adv.cuda(), got[3], up.cuda(), **more)
+    _close(back, torch.where(keep, up.double()[seq] * slope, 0.0), 2.0 ** -40, "policy grad_loss")
+    pair, reward, coef = vp.preference_forward(*dev, vp.Preference("squared", 0.3), ref.cuda())
+    R = 0.3 * total(ref.double() - loss.double())
+    _close(reward, R, 2.0 ** -45 * 0.3 * total(torch.full((T,), 3.0)), "reward")
+    z = R[0::2] - R[1::2]
+    _close(pair, ((z - 0.5) / 0.3) ** 2, 2.0 ** -38 * (1 + z.abs()), "pair_loss")
+    grad = vp.preference_backward(dev[1], dev[2], coef, up[:S // 2].cuda())
+    sign = torch.where(seq % 2 == 0, -1.0, 1.0).double()  # (float32 would round 0.3 to 0.3 (1 + 4e-8))
+    want = torch.where(keep, sign * 0.3 * (2 * (z - 0.5) / 0.09)[seq // 2] * up.double()[seq // 2], 0.0)
+    _close(grad, want, 1.01 * U * want.abs() + 2.0 ** -36, "preference grad_loss")
+
+
 def test_ratios_next_to_the_bounds():
     """Ratios one float32 step around each bound, and the bounds' neighbours in float64, fall on
     their side; a token without advantage has neither loss nor gradient."""
