@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "vpce_head.h"
+#include "vpce_lanes.h"
 
 namespace vpce {
 
@@ -71,9 +72,15 @@ struct Row {
 template <int LANES, int N, int W>
 __device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][W], int& turn) {
 #pragma unroll
-  for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1)
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
+  for (int k = 0; k < N; ++k) {
+    v[k] += lane_move<kSwap1>(v[k]);
+    v[k] += lane_move<kSwap2>(v[k]);
+    v[k] += lane_move<kHalfMirror>(v[k]);
+    if constexpr (LANES >= 16) v[k] += lane_move<kMirror>(v[k]);
+    if constexpr (LANES == 32) v[k] += __shfl_xor(v[k], 16);
+    if constexpr (LANES >= 64)
+      v[k] = (lane_read(v[k], 0) + lane_read(v[k], 16)) + (lane_read(v[k], 32) + lane_read(v[k], 48));
+  }
   if constexpr (LANES > 64) {
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
