@@ -6,6 +6,10 @@
 // wavefronts with a few 16-byte vectors of X in each lane; its sums are taken from there.
 // The variance is a second sum over the registers, around the mean, not a difference of
 // squares: a mean far above the spread costs no digits.
+//
+// MI355X, kernels alone: T = 32768, d = 2880, bfloat16 forward 67.9 us (5.6 TB/s), backward
+// 167 + 4.2 us (5.5 TB/s); T = 16384, d = 7168, float32 without a mean 159 us (5.9 TB/s) and
+// 254 + 4.1 us (5.5 TB/s); a 1 GiB copy runs at 5.1 to 5.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -407,8 +411,8 @@ struct Backward {
 // read (T = 32768, d = 2880, bfloat16: 256 workgroups 171 us, 512 173, 1024 196; float32
 // 195, 212, 231; T = 30000, d = 1200: 113, 75, 72 and 110, 80, 84).  No workgroup sums more
 // than 1024 rows in one chain.  Up to four rounds of rows one workgroup does it all and
-// the second launch is saved (T = 4, d = 4096: 9.2 us for the call instead of 12.3; T = 16
-// in one workgroup 20.4).
+// the second launch is saved (d = 4096, us a call: T = 4 so 7.7, T = 5 in two launches 11.0;
+// T = 16 in one workgroup took 20.4, 8 as long as in two).
 struct Parts {
   int rows, n;
   template <int LANES, int EL>

@@ -4,6 +4,14 @@
 // float32 inputs and outputs is float64: a ratio next to a clip bound falls on the side
 // it belongs to, e^q - q - 1 of a small q keeps its digits, and sums of any length are
 // as good as one rounding of their result.
+//
+// Bound: up to some 100000 tokens by launches and by the latency of a few dependent loads
+// (offsets, a sequence's values, partial sums); beyond by memory, 16 to 24 bytes a token in
+// the forward and 12 to 28 in the backward, and in the policy forward as much by its float64
+// arithmetic (174 vector instructions for 64 tokens).  MI355X, kernels alone: T = 32768 in 64
+// sequences, policy 4.6 + 1.9 us forward, 3.8 us backward; T = 4.2 M in 4096, 28.2 + 4.0 us
+// (3.6 TB/s) and 25.2 us (4.7 TB/s); preference, T = 4.0 M in 2500 pairs, 14.7 + 4.4 us
+// (4.4 TB/s) and 10.6 us (4.5 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -221,8 +229,8 @@ __device__ __forceinline__ bool sequence_sums(const SeqArgs& q, int s, double (&
 
 // e^x and e^x - 1: x = n ln 2 + r with |r| <= 0.3466, p = e^r - 1 by its series up to
 // r^11 / 11! (what is left out is below 2^-45 r), e^x = 2^n (1 + p).  e^x - 1 is p itself for
-// n = 0 and loses at most two bits to the difference otherwise.  Half the instructions of
-// the library's exp and expm1, which also carry their answers to the last bit.
+// n = 0 and loses at most two bits to the difference otherwise.  Fewer instructions than the
+// math library's exp and expm1, which carry their answers to the last bit of a double.
 __device__ __forceinline__ void exp_both(double x, double& e, double& em1) {
   const double y = fmin(fmax(x, -1100.0), 1100.0);
   const double n = rint(y * 1.4426950408889634);
@@ -517,6 +525,9 @@ bool forward(const Args& a, hipStream_t s) {
   const dim3 grid((unsigned)(p.chunks + 3) / 4);
   hipLaunchKernelGGL((chunk_kernel<Op, Args>), grid, dim3(256), 0, s, a);
   if (!launched_ok()) return false;
+  // a unit's parts side by side: a workgroup where there are many (one pair of 131071 tokens:
+  // 4.9 us instead of 5.6 in a wavefront), eight lanes where there are more units than
+  // wavefronts
   if (p.chunks >= 512 * (int64_t)units)
     launch_finish<Op, Args, 256>(a, units, s);
   else if (units <= 16384)
@@ -546,6 +557,9 @@ bool backward(const Op& op, hipStream_t s) {
 
 SeqPlan seq_plan(int T, int S) {
   SeqPlan p;
+  // Up to 2048 tokens the sixteen wavefronts of one workgroup, which then joins the sums in
+  // the same launch (policy forward, us a call / replayed in a graph: T = 2000, 16 sequences
+  // 8.3 / 6.4 instead of 11.5 / 5.7; T = 4000 8.8 / 8.7 instead of 11.5 / 5.7).
   const int most = T <= 2048 ? 16 : kWaves;
   p.chunk = 64 * std::max(1, (T + 64 * most - 1) / (64 * most));
   p.chunks = (T + p.chunk - 1) / p.chunk;
