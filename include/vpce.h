@@ -326,7 +326,8 @@ vp_status vp_pref_backward(const vp_sequences* seq, const int32_t* start, const 
  *   seq_loss_s = c_s sum_t l_t,   seq_kl_s = c_s sum_t kl_t
  * A token is clipped where the minimum is the clipped term alone (A > 0 and rho_t >
  * 1 + clip_high, or A < 0 and rho_t < 1 - clip_low; decided in float64): there the
- * first term has no gradient. */
+ * first term has no gradient.  (A mean over all tokens of the batch is the form without
+ * VP_SEQ_MEAN, with grad_seq = 1 / the sum of tokens.) */
 #define VP_ADV_PER_TOKEN 8u
 
 typedef struct {

@@ -379,12 +379,24 @@ template <class E, bool RMS>
 struct Forward {
   const NormArgs& a;
   hipStream_t s;
+  // A launch takes at most 2^30 threads (its size is a 32-bit number of threads: 2^23 rows
+  // of 1024 would not fit), and further rows further launches.
   template <int LANES, int EL>
   bool run() {
     using R = Row<E, LANES, EL>;
-    hipLaunchKernelGGL((norm_forward_kernel<E, RMS, LANES, EL>), dim3((unsigned)((a.T + R::ROWS - 1) / R::ROWS)),
-                       dim3(R::NT), 0, s, a);
-    return launched_ok();
+    constexpr int64_t kRows = (int64_t)R::ROWS * ((1 << 30) / R::NT);
+    for (int64_t t = 0; t < a.T; t += kRows) {
+      NormArgs b = a;
+      b.T = std::min(kRows, a.T - t);
+      b.X = (const typename E::storage*)a.X + t * a.d;
+      b.Y = (typename E::storage*)a.Y + t * a.d;
+      b.mean = RMS ? nullptr : a.mean + t;
+      b.rstd = a.rstd + t;
+      hipLaunchKernelGGL((norm_forward_kernel<E, RMS, LANES, EL>), dim3((unsigned)((b.T + R::ROWS - 1) / R::ROWS)),
+                         dim3(R::NT), 0, s, b);
+      if (!launched_ok()) return false;
+    }
+    return true;
   }
 };
 

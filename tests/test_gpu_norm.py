@@ -68,6 +68,8 @@ def _check_backward(X, gamma, mean, rstd, dY, got, base=None):
     _within(dX, dx, r * U * ((DEPTH + 10) * (m1 + xh.abs() * m2) + 10 * g.abs()) + 1e-44, "dX")
     T = X.shape[0]
     old = [0.0, 0.0] if base is None else [v.double().cpu() for v in base]
+    if dgamma is None:
+        return
     _within(dgamma, dg + old[0], (ROWS(T) + 4) * U * ((dy * xh).abs().sum(0) + (abs(old[0]))) + 1e-44, "dgamma")
     if dbeta is not None:
         _within(dbeta, db + old[1], (ROWS(T) + 1) * U * (dy.abs().sum(0) + abs(old[1])) + 1e-44, "dbeta")
@@ -154,6 +156,38 @@ def test_large_offset_keeps_the_spread():
     out = vp.layer_norm(X, gamma, beta, 1e-5)
     _check_forward(X, gamma, beta, 1e-5, False, out)
     _check_backward(X, gamma, out[1], out[2], dY, vp.layer_norm_backward(X, gamma, out[1], out[2], dY))
+
+
+@pytest.mark.parametrize("T, d, dtype", [
+    (300007, 8192, torch.bfloat16),   # more than 2^31 elements
+    (1048597, 4104, torch.float32),   # more rows than one launch of 2^30 threads has
+    (2 ** 23 - 256, 8, torch.bfloat16),  # the most rows
+])
+def test_large(T, d, dtype):
+    """Rows at the beginning, in the middle and at the end, and the sums over all rows, taken in
+    float64 on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    X = torch.empty(T, d, dtype=dtype, device="cuda").normal_(0.2, 1.0, generator=g)
+    gamma, beta = torch.linspace(0.5, 1.5, d, device="cuda").to(dtype), torch.linspace(-1, 1, d, device="cuda").to(dtype)
+    out = vp.layer_norm(X, gamma, beta)
+    rows = torch.cat([torch.arange(3), torch.arange(T // 2, T // 2 + 3), torch.arange(min(T, 2 ** 20) - 3, min(T, 2 ** 20 + 3)),
+                      torch.arange(T - 3, T)]).cuda()
+    _check_forward(X[rows], gamma, beta, 1e-5, False, [v[rows] for v in out])
+    mean, rstd = out[1:]
+    del out
+    dY = torch.empty(T, d, device="cuda").normal_(0.0, 1.0, generator=g)
+    dX, dgamma, dbeta = vp.layer_norm_backward(X, gamma, mean, rstd, dY)
+    want, mag = torch.zeros(2, d, dtype=torch.float64, device="cuda"), torch.zeros(2, d, dtype=torch.float64, device="cuda")
+    step = max(1, 2 ** 27 // d)
+    for a in range(0, T, step):
+        dy = dY[a:a + step].double()
+        p = (X[a:a + step].double() - mean[a:a + step, None]) * rstd[a:a + step, None] * dy
+        want += torch.stack([p.sum(0), dy.sum(0)])
+        mag += torch.stack([p.abs().sum(0), dy.abs().sum(0)])
+    # chains of at most 1024 rows of a lane, 32 rows side by side and 2^13 / 16 + 16 workgroups
+    bound = (1024 + 32 + 528 + 4) * U * mag
+    assert bool(((torch.stack([dgamma, dbeta]) - want).abs() <= bound).all())
+    _check_backward(X[rows], gamma, mean[rows], rstd[rows], dY[rows], (dX[rows], None, None))
 
 
 @pytest.mark.parametrize("T", [1, 300])

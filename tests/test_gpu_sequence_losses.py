@@ -159,7 +159,7 @@ def test_policy(layout, old, ref, per_token, kl_coef, mean):
     assert bool((back.cpu()[m["mask"]] == 0).all())
 
 
-@pytest.mark.parametrize("S, T", [(35000, 200003), (40000, 1500), (2 ** 22, 70000)])
+@pytest.mark.parametrize("S, T", [(35000, 200003), (40000, 1500), (2 ** 22, 70000), (8000, 2 ** 23 - 256)])
 def test_many_sequences(S, T):
     """More sequences than wavefronts, and many more sequences than tokens; sums by sequence from
     the plain form of each token."""
@@ -179,7 +179,7 @@ def test_many_sequences(S, T):
     dev = [v.cuda() for v in (loss, targets, start.int())]
     pol, more = vp.Policy(kl_coef=0.1), dict(old_loss=old.cuda(), ref_loss=ref.cuda())
     got = vp.policy_forward(*dev, pol, adv.cuda(), **more)
-    # at most 2^12 tokens a sequence, each below e^3 |A| + 0.1 e^3
+    # at most 2^15 tokens a sequence, each below e^3 |A| + 0.1 e^3
     _close(got[0], total(l), 2.0 ** -45 * total(21 * adv.double()[seq].abs() + 3), "seq_loss")
     _close(got[1], total(kl), 2.0 ** -45 * total(torch.full((T,), 21.0)), "seq_kl")
     assert torch.equal(got[2].cpu(), total(clipped).int()) and torch.equal(got[3].cpu(), total(keep).int())
