@@ -59,11 +59,13 @@ struct SeqPlan {
 SeqPlan seq_plan(int T, int S);
 constexpr int kMaxSeqSums = 3;  // of one slot
 
+// Arrays that a call leaves out are the loss in these, and what is read from them is not
+// used: every token's loads go out together, without a branch between them.
 struct PrefArgs {
   SeqArgs q;
   const float* loss;
-  const float* ref;  // or null
-  int32_t kind;
+  const float* ref;
+  int32_t has_ref, kind;
   double beta, margin, smoothing;
   float *pair_loss, *reward, *coef;
 };
@@ -71,9 +73,10 @@ struct PrefArgs {
 struct PolicyArgs {
   SeqArgs q;
   const float* loss;
-  const float *old, *ref;  // or null
-  const float* adv;
-  int32_t per_token;
+  const float *old, *ref;
+  const float* adv;      // [S], or unused
+  const float* adv_tok;  // [T], or unused
+  int32_t has_old, has_ref, per_token;
   double low, high;          // clip bounds of the ratio
   double log_low, log_high;  // and their logarithms
   double kl_coef;

@@ -95,9 +95,12 @@ vp_status policy_args(const vp_sequences* seq, const vp_policy* p, const int32_t
   *a = vpce::PolicyArgs{};
   a->q = seq_args(seq, start, targets);
   a->loss = loss;
-  a->old = old_loss;
-  a->ref = ref_loss;
+  a->old = old_loss ? old_loss : loss;
+  a->ref = ref_loss ? ref_loss : loss;
   a->adv = advantage;
+  a->adv_tok = per_token ? advantage : loss;
+  a->has_old = old_loss != nullptr;
+  a->has_ref = ref_loss != nullptr;
   a->per_token = per_token;
   a->low = 1.0 - p->clip_low;
   a->high = 1.0 + p->clip_high;
@@ -192,7 +195,8 @@ vp_status vp_pref_forward(const vp_sequences* seq, const vp_preference* pref, co
   vpce::PrefArgs a;
   a.q = seq_args(seq, start, targets, ws);
   a.loss = loss;
-  a.ref = ref_loss;
+  a.ref = ref_loss ? ref_loss : loss;
+  a.has_ref = ref_loss != nullptr;
   a.kind = pref->kind;
   a.beta = pref->beta;
   a.margin = pref->margin;

@@ -9,9 +9,9 @@
 // (offsets, a sequence's values, partial sums); beyond by memory, 16 to 24 bytes a token in
 // the forward and 12 to 28 in the backward, and in the policy forward as much by its float64
 // arithmetic (174 vector instructions for 64 tokens).  MI355X, kernels alone: T = 32768 in 64
-// sequences, policy 4.6 + 1.9 us forward, 3.8 us backward; T = 4.2 M in 4096, 28.2 + 4.0 us
-// (3.6 TB/s) and 25.2 us (4.7 TB/s); preference, T = 4.0 M in 2500 pairs, 14.7 + 4.4 us
-// (4.4 TB/s) and 10.6 us (4.5 TB/s).
+// sequences, policy 4.6 + 1.9 us forward, 3.6 us backward; T = 4.2 M in 4096, 28.3 + 4.0 us
+// (3.6 TB/s) and 21.4 us (5.5 TB/s); preference, T = 4.0 M in 2500 pairs, 14.9 + 4.5 us
+// (4.3 TB/s) and 9.3 us (5.2 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -144,7 +144,7 @@ __device__ __forceinline__ void chunk_sums(const Op& op, int c) {
   for (int b = t0; b < t1; b += 64) {
     const int e = min(b + 64, t1);
     raw = next;
-    if (e < t1) op.load(next, min(e + lane, t1 - 1));
+    op.load(next, min(e + lane, t1 - 1));
     const bool cut = e > end;
     const int mine = cut ? w.walk(q, b, e - 1) : s;
     double v[K];
@@ -305,7 +305,7 @@ struct PrefOp {
   __device__ __forceinline__ void load(Raw& r, int t) const {
     r.target = a.q.targets[t];
     r.loss = a.loss[t];
-    r.ref = a.ref ? a.ref[t] : 0.f;
+    r.ref = a.ref[t];
   }
   struct Seq {
     __device__ void wait() {}
@@ -313,7 +313,7 @@ struct PrefOp {
   __device__ __forceinline__ Seq open(int) const { return {}; }
   __device__ __forceinline__ void add(double (&v)[K], const Raw& r, const Seq&) const {
     if (r.target == a.q.ignore_index) return;
-    v[0] += (double)r.ref - (double)r.loss;
+    v[0] += (a.has_ref ? (double)r.ref : 0.0) - (double)r.loss;
     v[1] += 1.0;
   }
   static constexpr int PER_UNIT = 2;  // a unit is a pair
@@ -343,24 +343,24 @@ struct PolicyRaw {
 __device__ __forceinline__ void load_token(const PolicyArgs& a, PolicyRaw& r, int t) {
   r.target = a.q.targets[t];
   r.loss = a.loss[t];
-  r.old = a.old ? a.old[t] : 0.f;
-  r.ref = a.ref ? a.ref[t] : 0.f;
-  r.adv = a.per_token ? a.adv[t] : 0.f;
+  r.old = a.old[t];
+  r.ref = a.ref[t];
+  r.adv = a.adv_tok[t];
 }
 __device__ __forceinline__ PolicyToken policy_token(const PolicyArgs& a, const PolicyRaw& t, double adv) {
   PolicyToken r;
   const double nll = (double)t.loss;
   // (a NaN loss makes x a NaN without an old loss, too)
-  const double x = a.old ? (double)t.old - nll : (nll == nll ? 0.0 : nll);
+  const double x = a.has_old ? (double)t.old - nll : (nll == nll ? 0.0 : nll);
   r.clipped = adv > 0.0 ? x > a.log_high : adv < 0.0 ? x < a.log_low : false;
   double rho = 1.0 + x, unused;
-  if (a.old) exp_both(x, rho, unused);
+  if (a.has_old) exp_both(x, rho, unused);
   // no advantage: 0 also where rho is infinite
   const double gain = adv == 0.0 ? (x == x ? 0.0 : x) : rho * adv;
   r.loss = r.clipped ? -((adv > 0.0 ? a.high : a.low) * adv) : -gain;
   r.slope = r.clipped ? 0.0 : gain;
   r.kl = 0.0;
-  if (a.ref) {
+  if (a.has_ref) {
     const double q = nll - (double)t.ref;
     double em1;
     exp_both(q, unused, em1);
@@ -428,11 +428,10 @@ __global__ void __launch_bounds__(1024) small_kernel(Args args) {
   for (int unit = threadIdx.x; unit < args.q.S / Op::PER_UNIT; unit += 1024) op.template finish<1>(unit);
 }
 
-// Gradients: J tokens a lane, one where that does not fill the chip.  The more a token
-// brings with it, the fewer: 4 M tokens, J = 1 / 2 / 4: preference 14.9 / 11.4 / 9.9 us, policy
-// 27.5 / 25.2 / 27.2 us; 32768 tokens, policy 3.4 / 4.6 / 6.4 us.
+// Gradients: J tokens a lane, one where more would not fill the chip (4 M tokens, J = 1 / 2 /
+// 4: preference 15.2 / 11.4 / 9.1 us, policy 23.2 / 22.4 / 21.5 us; 32768 tokens, policy 3.4 /
+// 4.6 / 6.4 us).
 struct PrefGrad {
-  static constexpr int J = 4;
   SeqArgs q;
   const float* coef;
   const float* grad_pair;
@@ -448,7 +447,6 @@ struct PrefGrad {
   __device__ __forceinline__ float grad(const Raw&, const Seq& s) const { return s.grad; }
 };
 struct PolicyGrad {
-  static constexpr int J = 2;
   PolicyArgs a;
   SeqArgs q;
   float* grad_loss;
@@ -549,7 +547,7 @@ bool backward(const Op& op, hipStream_t s) {
   if (T <= 64 * kWaves)
     launch_grad<1>(op, s);
   else
-    launch_grad<Op::J>(op, s);
+    launch_grad<4>(op, s);
   return launched_ok();
 }
 
