@@ -266,9 +266,10 @@ vp_status vp_norm_backward(const vp_norm* norm, const void* X, const void* gamma
  * none).  A token counts if it belongs to a sequence and targets[t] != ignore_index:
  * what any other token's entry of a per-token array holds is not used (it may be NaN),
  * and its gradient is 0.  A counting token whose loss is NaN (an out-of-range target)
- * makes its sequence's results NaN, and no other's.  With n_s the counting tokens of sequence s, a sum over it is
- * weighted by c_s = 1, or with VP_SEQ_MEAN by c_s = 1 / n_s (0 where n_s == 0).
- * Sums are float64, results are rounded once to float32.
+ * makes the results of its sequence, or of its pair, NaN, and no others.
+ * With n_s the counting tokens of sequence s, a sum over it is weighted by c_s = 1, or
+ * with VP_SEQ_MEAN by c_s = 1 / n_s (0 where n_s == 0).  Sums are float64, results are
+ * rounded once to float32.
  *
  * Every offset is held against 0..T before it is used as one: wrong offsets never lead
  * outside an array.  A sequence whose own two offsets decrease or leave 0..T gets NaN

@@ -317,3 +317,88 @@ def test_plain_gradients_against_differences():
             e[j] = h
             diff = hp.norm_forward(X, gamma + e, None, 1e-3, rms)[0] - hp.norm_forward(X, gamma - e, None, 1e-3, rms)[0]
             assert abs(float((diff * dY).sum()) - 2 * h * float(dg[j])) <= 1e-8 * h
+
+
+# ---------------------------------------------------------------------------
+# How the kernels find the sequences of their tokens, in Python: 64 offsets at a time, whatever
+# they are.  Reads outside start[0..S] and sequences outside -1..S raise.
+class _Offsets:
+    BEHIND = 2 ** 31 - 1
+
+    def __init__(self, start):
+        self.start, self.S = start, len(start) - 1
+
+    def at(self, i):
+        assert 0 <= i <= self.S
+        return self.start[i]
+
+    def window(self, base):
+        assert base >= 0
+        return [self.at(base + k) if base + k <= self.S and self.S > 0 else self.BEHIND for k in range(64)]
+
+    def open(self, t):
+        lo, n, rounds = 0, self.S + 1, 0
+        while n > 64:
+            step = (n + 63) // 64
+            c = sum(lo + (k + 1) * step - 1 < lo + n and self.at(min(lo + (k + 1) * step - 1, self.S)) <= t
+                    for k in range(64))
+            lo, n, rounds = lo + c * step, min(step - 1, n - c * step), rounds + 1
+            assert n >= 0 and rounds <= 4
+        return lo, lo - 1 + sum(o <= t for o in self.window(lo))
+
+    def walk(self, base, first, last):
+        s, rounds = [base - 1] * (last - first + 1), 0
+        while True:
+            o = self.window(base)
+            s = [v + sum(x <= first for x in o) + sum(first < x <= last and x <= first + k for x in o)
+                 for k, v in enumerate(s)]
+            if o[63] > last:
+                return base, s
+            base, rounds = base + 64, rounds + 1
+            assert rounds <= self.S // 64 + 1
+
+
+def _ordered(g, S, T):
+    return sorted(int(v) for v in torch.randint(0, T + 1, (S + 1,), generator=g))
+
+
+def _disordered(g, S, T):
+    out = _ordered(g, S, T)
+    for i in torch.randint(0, S + 1, (max(1, S // 3),), generator=g).tolist():
+        out[i] = [-5, T + 9, 2 ** 31 - 1, -2 ** 31, 0, T // 2][int(torch.randint(0, 6, (1,), generator=g))]
+    return out
+
+
+@pytest.mark.parametrize("S", [0, 1, 2, 63, 64, 65, 200, 4096, 5000])
+@pytest.mark.parametrize("make", [_ordered, _disordered])
+def test_walk_over_offsets(S, make):
+    T = 700
+    for seed in range(3):
+        start = make(torch.Generator().manual_seed(100 * S + seed), S, T)
+        off = _Offsets(start)
+        for chunk in (64, 128):
+            slots = set()
+            for c in range(-(-T // chunk)):
+                t0, t1 = c * chunk, min(T, (c + 1) * chunk)
+                base, s = off.open(t0)
+                assert -1 <= s <= S
+                seen = []
+                for b in range(t0, t1, 64):
+                    base, mine = off.walk(base, b, min(b + 64, t1) - 1)
+                    assert all(-1 <= v <= S for v in mine)
+                    seen += mine
+                if make is _ordered and S > 0:
+                    want = torch.searchsorted(torch.tensor(start), torch.arange(t0, t1), right=True) - 1
+                    assert seen == want.tolist() and s == seen[0]
+                    parts = {c + v for v in set(seen) if 0 <= v < S}
+                    assert len(parts) == len({v for v in set(seen) if 0 <= v < S}) and not parts & slots
+                    slots |= parts
+            assert all(0 <= v < -(-T // chunk) + S for v in slots)
+
+
+@pytest.mark.parametrize("T, S", [(0, 0), (1, 2), (700, 0), (2048, 40), (2049, 40), (2 ** 20, 8), (2 ** 23 - 256, 2 ** 22)])
+def test_sequence_workspace_holds_every_part(T, S):
+    """Three sums for each chunk of tokens and each sequence."""
+    most = 16 if T <= 2048 else 16384
+    chunk = 64 * max(1, -(-T // (64 * most)))
+    assert vp.vp_seq_workspace_size(vp.Sequences(T, S)) >= 24 * (-(-T // chunk) + S)
