@@ -10,7 +10,7 @@
 // the forward and 12 to 28 in the backward, and in the policy forward as much by its float64
 // arithmetic (174 vector instructions for 64 tokens).  MI355X, kernels alone: T = 32768 in 64
 // sequences, policy 4.6 + 1.9 us forward, 3.6 us backward; T = 4.2 M in 4096, 28.3 + 4.0 us
-// (3.6 TB/s) and 21.4 us (5.5 TB/s); preference, T = 4.0 M in 2500 pairs, 14.9 + 4.5 us
+// (3.6 TB/s) and 21.4 us (5.5 TB/s); preference, T = 4.0 M in 2500 pairs, 14.9 + 3.9 us
 // (4.3 TB/s) and 9.3 us (5.2 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -210,18 +210,18 @@ __device__ __forceinline__ bool sequence_sums(const SeqArgs& q, int s, double (&
 #pragma unroll
       for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o);
   }
-  if constexpr (LANES > 64) {  // a workgroup
-    __shared__ double side[LANES / 64][K];
-    __syncthreads();  // (of the sequence before)
+  if constexpr (LANES > 64) {  // a workgroup of 256, or its halves
+    __shared__ double side[4][K];
+    const int first = threadIdx.x / LANES * (LANES / 64);
     if (lane_id() == 0)
 #pragma unroll
       for (int k = 0; k < K; ++k) side[threadIdx.x >> 6][k] = v[k];
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      v[k] = side[0][k];
+      v[k] = side[first][k];
 #pragma unroll
-      for (int w = 1; w < LANES / 64; ++w) v[k] += side[w][k];
+      for (int w = 1; w < LANES / 64; ++w) v[k] += side[first + w][k];
     }
   }
   return good;
@@ -316,16 +316,33 @@ struct PrefOp {
     v[0] += (a.has_ref ? (double)r.ref : 0.0) - (double)r.loss;
     v[1] += 1.0;
   }
-  static constexpr int PER_UNIT = 2;  // a unit is a pair
+  static constexpr int PER_UNIT = 2;  // a unit is a pair, its sequences side by side
   template <int LANES>
   __device__ __forceinline__ void finish(int pair) const {
-    double v[2][K], sum[2], n[2];
-    bool good = true;
+    constexpr int H = LANES / 2;
+    const int half = threadIdx.x / H & 1;
+    double v[K], sum[2], n[2];
+    bool good = sequence_sums<K, H>(a.q, 2 * pair + half, v);
+    if constexpr (LANES > 64) {
+      __shared__ double both[2][K];
+      __shared__ int fine[2];
+      if (threadIdx.x % H == 0) {
+        both[half][0] = v[0];
+        both[half][1] = v[1];
+        fine[half] = good;
+      }
+      __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      good &= sequence_sums<K, LANES>(a.q, 2 * pair + k, v[k]);
-      sum[k] = v[k][0];
-      n[k] = v[k][1];
+      for (int k = 0; k < 2; ++k) {
+        sum[k] = both[k][0];
+        n[k] = both[k][1];
+      }
+      good = fine[0] && fine[1];
+    } else {
+      const double s1 = __shfl_xor(v[0], H), n1 = __shfl_xor(v[1], H);
+      good = (int)good & __shfl_xor((int)good, H);
+      sum[0] = v[0], sum[1] = s1;  // (as the first half needs them)
+      n[0] = v[1], n[1] = n1;
     }
     if (threadIdx.x % LANES == 0) finish_pair(a, pair, sum, n, good);
   }
@@ -425,7 +442,9 @@ __global__ void __launch_bounds__(1024) small_kernel(Args args) {
   const Op op{args};
   chunk_sums(op, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
   __syncthreads();
-  for (int unit = threadIdx.x; unit < args.q.S / Op::PER_UNIT; unit += 1024) op.template finish<1>(unit);
+  constexpr int LANES = Op::PER_UNIT;
+  for (int unit = threadIdx.x / LANES; unit < args.q.S / Op::PER_UNIT; unit += 1024 / LANES)
+    op.template finish<LANES>(unit);
 }
 
 // Gradients: J tokens a lane, one where more would not fill the chip (4 M tokens, J = 1 / 2 /
@@ -516,7 +535,7 @@ bool forward(const Args& a, hipStream_t s) {
   if (q.S == 0) return true;
   const SeqPlan p = seq_plan(q.T, q.S);
   const int units = q.S / Op::PER_UNIT;
-  if (p.chunks <= 16 && units <= 2048) {  // (a workgroup's threads take two units at most)
+  if (p.chunks <= 16 && units <= 2048) {  // (a thread takes a few units at most)
     hipLaunchKernelGGL((small_kernel<Op, Args>), dim3(1), dim3(1024), 0, s, a);
     return launched_ok();
   }
@@ -524,7 +543,7 @@ bool forward(const Args& a, hipStream_t s) {
   hipLaunchKernelGGL((chunk_kernel<Op, Args>), grid, dim3(256), 0, s, a);
   if (!launched_ok()) return false;
   // a unit's parts side by side: a workgroup where there are many (one pair of 131071 tokens:
-  // 4.9 us instead of 5.6 in a wavefront), eight lanes where there are more units than
+  // 4.0 us instead of 5.5 in a wavefront), eight lanes where there are more units than
   // wavefronts
   if (p.chunks >= 512 * (int64_t)units)
     launch_finish<Op, Args, 256>(a, units, s);
