@@ -92,7 +92,7 @@ def policy_tokens(loss, old, ref, adv, low, high, kl_coef):
     return l, kl, clipped, slope
 
 
-def policy(loss, targets, start, adv, old, ref, ignore, mean, low, high, kl_coef, grad_seq=None):
+def policy(loss, targets, start, adv, old, ref, ignore, mean, low, high, kl_coef, grad_seq=None, per_token=False):
     """(seq_loss, seq_kl, clipped, tokens) and, with grad_seq, the gradient."""
     d = lambda v: None if v is None else v.double().cpu()  # noqa: E731
     loss, old, ref, adv, targets = d(loss), d(old), d(ref), d(adv), targets.cpu()
@@ -101,7 +101,7 @@ def policy(loss, targets, start, adv, old, ref, ignore, mean, low, high, kl_coef
     grad = torch.zeros(T, dtype=torch.float64)
     for s, (a, b) in enumerate(spans(start, T)):
         at = torch.arange(a, b)[targets[a:b] != ignore]
-        A = adv[at] if adv.numel() == T and adv.numel() != S else adv[s].expand(len(at))
+        A = adv[at] if per_token else adv[s].expand(len(at))
         l, kl, clipped, slope = policy_tokens(loss[at], None if old is None else old[at],
                                               None if ref is None else ref[at], A, low, high, kl_coef)
         c = weight(len(at), mean)

@@ -129,7 +129,7 @@ def test_preference_step(dtype):
     want = 0.95 * torch.nn.functional.softplus(-z) + 0.05 * torch.nn.functional.softplus(z)
     (want.sum() * 0.5).backward()
     bar = 1e-5 if dtype == torch.float32 else 2e-3
-    worst = bar * max(1.0, float(nll.max())) * 203 * 0.2
+    worst = bar * max(1.0, float(nll.detach().max())) * 203 * 0.2
     assert bool(((pair.cpu() - want).abs() <= worst).all())
     _compare(dtype, got, leaves, "preference")
 

@@ -69,8 +69,10 @@ LAYOUTS = {
     "one off whole blocks": ([255, 257, 1023, 1025], 0, 1),
     "single tokens": ([1] * 1200, 0, 3),
     "tens of tokens": (_spread(150, 4000, 1), 0, 17),
-    "one workgroup": (_spread(8, 4096, 2), 0, 0),
-    "just above": (_spread(8, 4097, 2), 0, 0),
+    "one workgroup": (_spread(8, 2048, 2), 0, 0),
+    "just above": (_spread(8, 2049, 2), 0, 0),
+    "4096 tokens": (_spread(8, 4096, 2), 0, 0),
+    "4097 tokens": (_spread(8, 4097, 2), 0, 0),
     "a long one among short ones": ([3, 5, 150000, 1, 0, 40, 70001, 2], 2, 5),
     "many of a wide spread": (_spread(3000, 400000, 3), 0, 1000),
     "empty ones inside": ([5] + [0] * 700 + [900] + [0] * 3001 + [1, 2, 0], 0, 0),
@@ -136,12 +138,11 @@ def _policy_args(m, old, ref, per_token, mean):
 def test_policy(layout, old, ref, per_token, kl_coef, mean):
     m = _make(*LAYOUTS[layout])
     adv, o, r = _policy_args(m, old, ref, per_token, mean)
-    if per_token and m["T"] == m["S"]:
-        pytest.skip("one advantage per token is one per sequence here")
     pol = vp.Policy(0.08, 0.1, kl_coef, per_token)
     got = vp.policy_forward(m["loss"], m["targets"], m["start"], pol, adv, o, r, IGNORE, mean)
     g = torch.linspace(-1, 2, m["S"])
-    want, grad = hp.policy(m["loss"], m["targets"], m["start"].cpu(), adv, o, r, IGNORE, mean, 0.08, 0.1, kl_coef, g)
+    want, grad = hp.policy(m["loss"], m["targets"], m["start"].cpu(), adv, o, r, IGNORE, mean, 0.08, 0.1, kl_coef, g,
+                           per_token)
     n = want[3].double().clamp_min(1)
     c = 1 / n if mean else torch.ones_like(n)
     # |l_t| <= e^|x| |A| + kl_coef kl with |x|, |q| <= 0.2: below 2 |A| + 0.1, and kl below 0.1;
