@@ -86,7 +86,8 @@ class Sequences:
 
 
 class Preference:
-    """A ``vp_preference``: kind ("logistic" or "squared"), beta, margin and label smoothing."""
+    """A ``vp_preference``: kind ("logistic" or "squared"), beta, margin and label smoothing (0..1/2;
+    the squared form has none, and calls with it leave the value unused)."""
 
     def __init__(self, kind: str = "logistic", beta: float = 0.1, margin: float = 0.0, smoothing: float = 0.0):
         kinds = {"logistic": VP_PREF_LOGISTIC, "squared": VP_PREF_SQUARED}
@@ -199,10 +200,18 @@ def vp_seq_workspace_size(seq: Sequences) -> int:
     return int(n.value)
 
 
+def _preference_ref(pref: Preference):
+    """What the C entry takes for `pref`: with the squared form it accepts no smoothing but 0."""
+    c = pref.c
+    if c.kind == VP_PREF_SQUARED and 0.0 < c.smoothing <= 0.5:
+        return ctypes.byref(vp_preference(kind=c.kind, beta=c.beta, margin=c.margin))
+    return pref.ref
+
+
 def vp_pref_forward(seq: Sequences, pref: Preference, start, targets, loss, ref_loss, pair_loss, reward, coef, ws,
                     stream=None) -> None:
     """pair_loss [S/2], reward [S] and coef [S] of S/2 pairs.  ref_loss may be None."""
-    _call("vp_pref_forward", (seq.ref, pref.ref), seq.pref_forward_spec,
+    _call("vp_pref_forward", (seq.ref, _preference_ref(pref)), seq.pref_forward_spec,
           (start, targets, loss, ref_loss, pair_loss, reward, coef), stream, ws, lambda: vp_seq_workspace_size(seq))
 
 
