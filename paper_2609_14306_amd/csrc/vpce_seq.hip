@@ -539,9 +539,11 @@ bool forward(const Args& a, hipStream_t s) {
     hipLaunchKernelGGL((small_kernel<Op, Args>), dim3(1), dim3(1024), 0, s, a);
     return launched_ok();
   }
-  const dim3 grid((unsigned)(p.chunks + 3) / 4);
-  hipLaunchKernelGGL((chunk_kernel<Op, Args>), grid, dim3(256), 0, s, a);
-  if (!launched_ok()) return false;
+  if (p.chunks > 0) {  // (no tokens: sequences without a part)
+    const dim3 grid((unsigned)(p.chunks + 3) / 4);
+    hipLaunchKernelGGL((chunk_kernel<Op, Args>), grid, dim3(256), 0, s, a);
+    if (!launched_ok()) return false;
+  }
   // a unit's parts side by side: a workgroup where there are many (one pair of 131071 tokens:
   // 4.0 us instead of 5.5 in a wavefront), eight lanes where there are more units than
   // wavefronts

@@ -4,6 +4,7 @@
 //   ordered     outputs against plain loops in double, for layouts of every kind
 //   disordered  offsets that decrease or leave the tokens: NaN for the sequences that they bound,
 //               every gradient written, nothing outside the arrays touched
+//   no tokens   empty sequences alone, more of them than one workgroup takes among them
 #include <sys/mman.h>
 
 #include <random>
@@ -269,10 +270,25 @@ static bool longer() {
   return true;
 }
 
+// Sequences without any tokens, from a few to more than one workgroup takes.
+static bool no_tokens() {
+  unsigned seed = 0;
+  for (int S : {0, 1, 2, 2048, 2049, 2050, 4096, 4098, 20000})
+    for (int wrong = 0; wrong < (S ? 2 : 1); ++wrong) {
+      snprintf(what, sizeof what, "no tokens, S %d%s", S, wrong ? ", wrong offsets" : "");
+      std::vector<int> v(S + 1, 0);
+      if (wrong) v[S / 2] = -1, v[S] = 9;
+      const Options o = {(seed & 1) != 0, (seed & 2) == 0, (seed & 4) == 0, (seed & 8) != 0, (int)(seed / 2 % 2)};
+      if (!run(0, v, o, seed++)) return false;
+    }
+  return true;
+}
+
 int main(int argc, char** argv) {
   const bool ok = argc > 1 && (!strcmp(argv[1], "ordered")      ? all(false)
                                : !strcmp(argv[1], "disordered") ? all(true)
                                : !strcmp(argv[1], "longer")     ? longer()
+                               : !strcmp(argv[1], "no tokens")  ? no_tokens()
                                                                 : false);
   printf("%s, %ld launches\n", ok ? "ok" : "FAILED", cpu::launches);
   return ok ? 0 : 1;

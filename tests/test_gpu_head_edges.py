@@ -1,4 +1,6 @@
 """Calls at the edges of what the operators around the projection allow, on the GPU."""
+import math
+
 import pytest
 import torch
 
@@ -15,3 +17,27 @@ def test_squared_preference_with_a_smoothing_that_it_does_not_use():
     want = vp.preference_forward(loss, targets, start, vp.Preference("squared", 0.3, 0.1), ref)
     got = vp.preference_forward(loss, targets, start, vp.Preference("squared", 0.3, 0.1, 0.1), ref)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("S", [2, 2049, 2050, 4098, 40000])
+def test_sequences_without_tokens(S):
+    """No tokens at all, in more sequences than one workgroup takes: sums of 0 and the loss of a
+    pair at -margin."""
+    none, ids = torch.empty(0, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda")
+    start, adv = torch.zeros(S + 1, dtype=torch.int32, device="cuda"), torch.ones(S, device="cuda")
+    for mean in (False, True):
+        out = vp.policy_forward(none, ids, start, vp.Policy(kl_coef=0.1), adv, none, none, mean=mean)
+        assert all(bool((v == 0).all()) for v in out)
+        grad = vp.policy_backward(none, ids, start, vp.Policy(kl_coef=0.1), adv, out[3], adv, none, none, mean=mean)
+        assert grad.numel() == 0
+        if S % 2 == 0:
+            pair, reward, coef = vp.preference_forward(none, ids, start, vp.Preference(beta=0.5, margin=0.75), none,
+                                                       mean=mean)
+            assert bool((reward == 0).all())
+            want = math.log1p(math.exp(0.75))
+            assert bool(((pair.double() - want).abs() <= want * 2.0 ** -24).all())
+            # a sequence without tokens weighs 1, or 0 in the mean
+            half = 0.0 if mean else 0.5 / (1 + math.exp(-0.75))
+            sign = torch.tensor([-1.0, 1.0], device="cuda").repeat(S // 2)
+            assert bool(((coef.double() * -sign - half).abs() <= half * 2.0 ** -24 * 1.01).all())
+            assert vp.preference_backward(ids, start, coef, adv[:S // 2].contiguous()).numel() == 0
