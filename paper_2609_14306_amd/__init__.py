@@ -459,7 +459,7 @@ from .head import (HeadNorm, Norm, Policy, Preference, Sequences, layer_norm,  #
                    layer_norm_backward, policy_backward, policy_forward, preference_backward,
                    preference_forward, vp_norm_backward, vp_norm_forward, vp_norm_workspace_size,
                    vp_policy_backward, vp_policy_forward, vp_pref_backward, vp_pref_forward,
-                   vp_seq_workspace_size)
+                   vp_seq_workspace_size, _check_norm_grads)
 
 
 def problem_for(H, W_shards, ignore_index: int = -100, order=None, flags: int = 0,
@@ -532,16 +532,21 @@ def backward(H, W_shards: List, targets, lse, grad_loss, ignore_index: int = -10
 
     With `norm` (as given to `forward`): (dH, [dW_p], dgamma, dbeta) with the gradient of the
     norm's input as dH, written over that of its result; the norm is recomputed.  dbeta is None
-    without a beta.  `dnorm`: (dgamma, dbeta) to write, or with `accumulate` to add to."""
+    without a beta.  `dnorm`: (dgamma, dbeta) to write, or with `accumulate` to add to; what is
+    wrong with them is refused in front of all work, and so is a `dnorm` without a `norm`."""
     import torch
+    if norm is None and dnorm is not None:
+        raise ValueError("dnorm: there is no norm that it is of")
     if norm is not None:
         X = H
+        dgamma, dbeta = (None, None) if dnorm is None else dnorm
+        add = accumulate and dnorm is not None
+        _check_norm_grads(X, norm.beta is not None, dgamma, dbeta, add)
         H, mean, rstd = layer_norm(X, norm.gamma, norm.beta, norm.eps, norm.rms)
         dH, dW_shards = backward(H, W_shards, targets, lse, grad_loss, ignore_index, order, dW_shards,
                                  accumulate, ws, strip_elems)
-        dgamma, dbeta = (None, None) if dnorm is None else dnorm
         dH, dgamma, dbeta = layer_norm_backward(X, norm.gamma, mean, rstd, dH, norm.beta is not None, dH,
-                                                dgamma, dbeta, accumulate and dnorm is not None)
+                                                dgamma, dbeta, add)
         return dH, dW_shards, dgamma, dbeta
     flags = VP_ACCUMULATE_DW if accumulate else 0
     prob = problem_for(H, W_shards, ignore_index, order, flags, strip_elems)

@@ -10,9 +10,9 @@ from __future__ import annotations
 import ctypes
 from functools import cached_property
 
-from . import (VP_ACCUMULATE_DW, VP_ADV_PER_TOKEN, VP_ERR_WORKSPACE, VP_NORM_RMS, VP_PREF_LOGISTIC,
-               VP_PREF_SQUARED, VP_SEQ_MEAN, _check, _dtype_code, _need, _need_ws, _same_device, _torch_dtype,
-               load_library, vp_norm, vp_policy, vp_preference, vp_sequences)
+from . import (VP_ACCUMULATE_DW, VP_ADV_PER_TOKEN, VP_ERR_ALIGN, VP_ERR_WORKSPACE, VP_NORM_RMS,
+               VP_PREF_LOGISTIC, VP_PREF_SQUARED, VP_SEQ_MEAN, VpError, _check, _dtype_code, _need, _need_ws,
+               _same_device, _torch_dtype, load_library, vp_norm, vp_policy, vp_preference, vp_sequences)
 
 
 class Norm:
@@ -256,13 +256,27 @@ def layer_norm(X, gamma, beta=None, eps: float = 1e-5, rms: bool = False):
     return Y, mean, rstd
 
 
+def _check_norm_grads(X, bias, dgamma, dbeta, accumulate) -> None:
+    """What a norm backward refuses of the given dgamma and dbeta (None: none given), for callers
+    that have other work in front of it."""
+    import torch
+    if accumulate and (dgamma is None or (bias and dbeta is None)):
+        raise ValueError("accumulate: dgamma (and dbeta) to add to are needed")
+    named = [(n, t) for n, t in (("dgamma", dgamma), ("dbeta", dbeta if bias else None)) if t is not None]
+    for name, t in named:
+        _need(t, name, torch.float32, (X.shape[1],))
+        if t.data_ptr() % 16 != 0:
+            raise VpError(VP_ERR_ALIGN, name)
+    if named:
+        _same_device([("X", X)] + named)
+
+
 def layer_norm_backward(X, gamma, mean, rstd, dY, bias: bool = True, dX=None, dgamma=None, dbeta=None,
                         accumulate: bool = False, ws=None):
     """(dX, dgamma, dbeta) float32 from dY float32 [T, d]; mean None means the RMS form, and
     `bias` False no dbeta (None).  dX may be dY; with `accumulate` the given dgamma and dbeta are
     added to."""
-    if accumulate and (dgamma is None or (bias and dbeta is None)):
-        raise ValueError("accumulate: dgamma (and dbeta) to add to are needed")
+    _check_norm_grads(X, bias, dgamma, dbeta, accumulate)
     norm = Norm(X.shape[0], X.shape[1], _dtype_code(X), 0.0, mean is None, accumulate)
     dX = _f32(norm.T, norm.d, like=X) if dX is None else dX
     dgamma = _f32(norm.d, like=X) if dgamma is None else dgamma

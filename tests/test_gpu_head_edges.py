@@ -41,3 +41,20 @@ def test_sequences_without_tokens(S):
             sign = torch.tensor([-1.0, 1.0], device="cuda").repeat(S // 2)
             assert bool(((coef.double() * -sign - half).abs() <= half * 2.0 ** -24 * 1.01).all())
             assert vp.preference_backward(ids, start, coef, adv[:S // 2].contiguous()).numel() == 0
+
+
+@pytest.mark.parametrize("what", ["dbeta missing", "dgamma's shape", "dbeta's type", "unaligned", "on the CPU"])
+def test_wrong_norm_gradients_leave_dw_alone(what):
+    """`backward` refuses a dnorm before it adds to anything."""
+    d = 64
+    f = lambda *s: torch.rand(*s, device="cuda")  # noqa: E731
+    X, W, targets = f(20, d), [f(100, d)], torch.zeros(20, dtype=torch.int64, device="cuda")
+    norm = vp.HeadNorm(f(d), f(d))
+    lse = vp.forward(X, W, targets, norm=norm)[1]
+    dW = [torch.full((100, d), 3.0, device="cuda")]
+    dnorm = {"dbeta missing": (f(d), None), "dgamma's shape": (f(d + 8), f(d)), "dbeta's type": (f(d), f(d).double()),
+             "unaligned": (f(d + 1)[1:], f(d)), "on the CPU": (f(d), f(d).cpu())}[what]
+    with pytest.raises((ValueError, vp.VpError)):
+        vp.backward(X, W, targets, lse, f(20), norm=norm, dW_shards=dW, accumulate=True, dnorm=dnorm)
+    torch.cuda.synchronize()
+    assert bool((dW[0] == 3).all())
