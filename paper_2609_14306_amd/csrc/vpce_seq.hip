@@ -227,11 +227,13 @@ __device__ __forceinline__ bool sequence_sums(const SeqArgs& q, int s, double (&
   return good;
 }
 
-// e^x and e^x - 1: x = n ln 2 + r with |r| <= 0.3466, p = e^r - 1 by its series up to
-// r^11 / 11! (what is left out is below 2^-45 r), e^x = 2^n (1 + p).  e^x - 1 is p itself for
-// n = 0 and loses at most two bits to the difference otherwise.  Fewer instructions than the
-// math library's exp and expm1, which carry their answers to the last bit of a double.
-__device__ __forceinline__ void exp_both(double x, double& e, double& em1) {
+// e^x, e^x - 1 and e^x - 1 - x: x = n ln 2 + r with |r| <= 0.3466, p = e^r - 1 = r + tail by its
+// series up to r^11 / 11! (what is left out is below 2^-45 r and 2^-42 of the tail), e^x =
+// 2^n (1 + p).  For n = 0 the other two are p and the tail themselves, so a small x keeps the
+// digits of its x^2 / 2; otherwise each loses at most five bits to its difference (|x| >= 0.3466:
+// e^x - 1 - x >= 0.05).  Fewer instructions than the math library's exp and expm1, which carry
+// their answers to the last bit of a double.
+__device__ __forceinline__ void exp_both(double x, double& e, double& em1, double& rest) {
   const double y = fmin(fmax(x, -1100.0), 1100.0);
   const double n = rint(y * 1.4426950408889634);
   double r = fma(n, -0.6931471805599453, y);
@@ -246,10 +248,12 @@ __device__ __forceinline__ void exp_both(double x, double& e, double& em1) {
   p = fma(p, r, 1.0 / 24.0);
   p = fma(p, r, 1.0 / 6.0);
   p = fma(p, r, 0.5);
-  p = fma(p * r, r, r);
+  const double half = p * r, tail = half * r;
+  p = fma(half, r, r);
   e = ldexp(1.0 + p, (int)n);
   em1 = n == 0.0 ? p : e - 1.0;
-  if (!(x == x)) e = em1 = x;
+  rest = n == 0.0 ? tail : em1 == __builtin_inf() ? em1 : em1 - x;  // (no difference of infinities)
+  if (!(x == x)) e = em1 = rest = x;
 }
 
 // log(1 + e) for 0 <= e <= 1: 2 atanh(u), u = e / (2 + e) <= 1/3, by its series up to
@@ -274,8 +278,8 @@ __device__ void finish_pair(const PrefArgs& a, int pair, const double (&sum)[2],
   const double z = reward[0] - reward[1] - a.margin;
   double loss, slope;
   if (a.kind == VP_PREF_LOGISTIC) {
-    double e, unused;
-    exp_both(-fabs(z), e, unused);
+    double e, unused[2];
+    exp_both(-fabs(z), e, unused[0], unused[1]);
     const double l = log_1_plus(e);
     const double pos = 1.0 / (1.0 + e), neg = e * pos;  // sigmoid of |z| and of -|z|
     loss = (1.0 - a.smoothing) * (l + fmax(-z, 0.0));
@@ -370,18 +374,16 @@ __device__ __forceinline__ PolicyToken policy_token(const PolicyArgs& a, const P
   // (a NaN loss makes x a NaN without an old loss, too)
   const double x = a.has_old ? (double)t.old - nll : (nll == nll ? 0.0 : nll);
   r.clipped = adv > 0.0 ? x > a.log_high : adv < 0.0 ? x < a.log_low : false;
-  double rho = 1.0 + x, unused;
-  if (a.has_old) exp_both(x, rho, unused);
+  double rho = 1.0 + x, unused[2];
+  if (a.has_old) exp_both(x, rho, unused[0], unused[1]);
   // no advantage: 0 also where rho is infinite
   const double gain = adv == 0.0 ? (x == x ? 0.0 : x) : rho * adv;
   r.loss = r.clipped ? -((adv > 0.0 ? a.high : a.low) * adv) : -gain;
   r.slope = r.clipped ? 0.0 : gain;
   r.kl = 0.0;
   if (a.has_ref) {
-    const double q = nll - (double)t.ref;
     double em1;
-    exp_both(q, unused, em1);
-    r.kl = em1 == __builtin_inf() ? em1 : em1 - q;  // (q infinite: no difference of infinities)
+    exp_both(nll - (double)t.ref, unused[0], em1, r.kl);
     if (a.kl_coef > 0.0) {
       r.loss += a.kl_coef * r.kl;
       r.slope += a.kl_coef * em1;

@@ -1,5 +1,6 @@
 """Calls at the edges of what the operators around the projection allow, on the GPU."""
 import math
+from fractions import Fraction
 
 import pytest
 import torch
@@ -58,3 +59,35 @@ def test_wrong_norm_gradients_leave_dw_alone(what):
         vp.backward(X, W, targets, lse, f(20), norm=norm, dW_shards=dW, accumulate=True, dnorm=dnorm)
     torch.cuda.synchronize()
     assert bool((dW[0] == 3).all())
+
+
+def _kl(q):
+    """e^q - q - 1 without a difference of nearly equal numbers."""
+    if abs(q) > 1:
+        return math.expm1(q) - q
+    total, term = Fraction(0), Fraction(q)
+    for k in range(2, 30):
+        term = term * Fraction(q) / k
+        total += term
+    return float(total)
+
+
+def test_small_log_ratios_keep_their_digits():
+    """The KL term and its gradient of log ratios down to where float32 ends: each is one rounding
+    of the exact value (2^-24), for which the float64 arithmetic has 2^-40 to spend."""
+    q = [s * m * 10.0 ** -k for k in range(22) for m in (1.0, 3.4657, 3.466) for s in (1, -1)] + [7.5, -30.0, 80.0]
+    loss = torch.tensor([max(v, 0.0) for v in q])
+    ref = torch.tensor([max(-v, 0.0) for v in q])
+    T = len(q)
+    exact = [a - b for a, b in zip(loss.double().tolist(), ref.double().tolist())]
+    targets = torch.zeros(T, dtype=torch.int64, device="cuda")
+    start = torch.arange(T + 1, dtype=torch.int32, device="cuda")
+    pol, adv, one = vp.Policy(kl_coef=0.5), torch.zeros(T, device="cuda"), torch.ones(T, device="cuda")
+    seq_loss, kl, _, tokens = vp.policy_forward(loss.cuda(), targets, start, pol, adv, None, ref.cuda())
+    grad = vp.policy_backward(loss.cuda(), targets, start, pol, adv, tokens, one, None, ref.cuda())
+    for got, want in ((kl, [_kl(v) for v in exact]), (seq_loss, [0.5 * _kl(v) for v in exact]),
+                      (grad, [0.5 * math.expm1(v) for v in exact])):
+        want = torch.tensor(want, dtype=torch.float64)
+        err = (got.double().cpu() - want).abs()
+        bad = err > (2.0 ** -24 + 2.0 ** -40) * want.abs() + 2.0 ** -149
+        assert not bool(bad.any()), [(exact[i], float(got[i]), float(want[i])) for i in bad.nonzero()[:4, 0].tolist()]
