@@ -5,7 +5,12 @@
 // ((e + 8) T d bytes).  So a row is loaded once and stays in registers, spread over W
 // wavefronts with a few 16-byte vectors of X in each lane; its sums are taken from there.
 // The variance is a second sum over the registers, around the mean, not a difference of
-// squares: a mean far above the spread costs no digits.
+// squares.  A float32 mean far above the spread is itself some roundings off, which the
+// spread would see: in a row whose mean is more than 4 spreads away the distances' own mean
+// (`left`, a third sum: 1% of the time, T = 32768, d = 2880) takes what is left of it out of
+// Y, rstd and the stored mean; nearer ones have roundings of the mean no larger than those of
+// the distances.  The backward has the mean in float32 alone: one rounding of it is what xh of
+// such a row is off by there.
 //
 // MI355X, kernels alone: T = 32768, d = 2880, bfloat16 forward 67.9 us (5.6 TB/s), backward
 // 167 + 4.2 us (5.5 TB/s); T = 16384, d = 7168, float32 without a mean 159 us (5.9 TB/s) and
@@ -119,7 +124,7 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(N
     E::unpack(i < nvec ? x[i] : make_uint4(0, 0, 0, 0), f[k]);
   }
   const float inv_d = 1.f / (float)a.d;
-  float mean = 0.f;
+  float mean = 0.f, left = 0.f;
   if (!RMS) {
     float s[1] = {0.f};
 #pragma unroll
@@ -140,7 +145,19 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(N
     }
   }
   row_sum<LANES>(s, red, turn);
-  const float rstd = 1.f / sqrtf(s[0] * inv_d + a.eps);
+  float var = s[0] * inv_d;
+  if (!RMS && mean * mean > 16.f * var) {  // (the same for every lane of the row)
+    float c[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) c[0] += f[k][j];
+    row_sum<LANES>(c, red, turn);
+    left = c[0] * inv_d;
+    var = __builtin_fmaf(-left, left, var);
+    var = var < 0.f ? 0.f : var;
+  }
+  const float rstd = 1.f / sqrtf(var + a.eps), shift = -left * rstd;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int i = lane + k * R::LANES;
@@ -150,7 +167,7 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(N
       if (a.beta) E::unpack(((const uint4*)a.beta)[i], be);
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float xh = f[k][j] * rstd;
+        const float xh = RMS ? f[k][j] * rstd : __builtin_fmaf(f[k][j], rstd, shift);
         ga[j] = a.beta ? __builtin_fmaf(xh, ga[j], be[j]) : xh * ga[j];
       }
       y[i] = E::pack(ga);
@@ -158,7 +175,7 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(N
   }
   if (lane == 0) {
     a.rstd[t] = rstd;
-    if (!RMS) a.mean[t] = mean;
+    if (!RMS) a.mean[t] = mean + left;
   }
 }
 

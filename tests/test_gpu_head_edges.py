@@ -5,6 +5,7 @@ from fractions import Fraction
 import pytest
 import torch
 
+import head_plain as hp
 import paper_2609_14306_amd as vp
 
 pytestmark = pytest.mark.gpu
@@ -91,3 +92,50 @@ def test_small_log_ratios_keep_their_digits():
         err = (got.double().cpu() - want).abs()
         bad = err > (2.0 ** -24 + 2.0 ** -40) * want.abs() + 2.0 ** -149
         assert not bool(bad.any()), [(exact[i], float(got[i]), float(want[i])) for i in bad.nonzero()[:4, 0].tolist()]
+
+
+@pytest.mark.parametrize("T, d", [(50, 2880), (20, 7168), (9, 16384), (60, 1000), (300, 64), (40, 264)])
+@pytest.mark.parametrize("dtype, offset", [(torch.bfloat16, 30.0), (torch.bfloat16, 3.9), (torch.float32, 1000.0),
+                                           (torch.float32, 4.1), (torch.float32, -3.9)])
+def test_offset_above_the_spread(T, d, dtype, offset):
+    """Rows whose mean is up to 1000 times their spread (float32) or 30 times (bfloat16, whose
+    values are 1/256 of the mean apart).  With u = 2^-24 and chains of at most DEPTH = 144
+    additions: the mean of the first sum is off by e0 = 146 u mean|x|, the distances c from it by
+    u |c|, and what is left of the mean in them, taken from their own sum where the mean is more
+    than 4 spreads away, by e = 146 u mean|c|.  So Y does not depend on how far away the mean is:
+    its centre is off by e (e0 within 4 spreads) + 2 u |c| and its rstd by 77 u, relative, and
+    half of e0^2 / var where that is left in it; the mean by u |mean| and e or e0."""
+    u, depth = 2.0 ** -24, 144
+    g = torch.Generator().manual_seed(T + d)
+    X = (offset + torch.randn(T, d, generator=g)).to(dtype)
+    gamma, beta = (1 + 0.2 * torch.randn(d, generator=g)).to(dtype), torch.randn(d, generator=g).to(dtype)
+    Y, mean, rstd = (v.double().cpu() for v in vp.layer_norm(X.cuda(), gamma.cuda(), beta.cuda(), 1e-5))
+    y, mu, r = hp.norm_forward(X, gamma, beta, 1e-5, False)
+    x, ga = X.double(), gamma.double().abs()
+    e0 = (depth + 2) * u * x.abs().mean(1)
+    c = (x - mu[:, None]).abs() + e0[:, None]
+    far = mu ** 2 > 16.01 / r ** 2
+    e = torch.where(far, (depth + 2) * u * c.mean(1), e0)
+    e_r = 77 * u + torch.where(far, 0.0, 0.5 * e0 ** 2 * r ** 2)
+    assert bool(((mean - mu).abs() <= 1.01 * (u * mu.abs() + e)).all())
+    assert bool(((rstd - r).abs() <= e_r * r).all())
+    xh = c * r[:, None]
+    bound = ga * ((r * e)[:, None] + xh * (e_r + 8 * u)[:, None]) + 2 * u * (ga * xh + beta.double().abs())
+    half = torch.finfo(dtype).eps / 2
+    err = (Y - y).abs() - (bound * (1 + half) + half * y.abs())
+    assert bool((err <= 0).all()), float(err.max())
+
+
+@pytest.mark.parametrize("value", [0.1, 1000.1, -3e4])
+@pytest.mark.parametrize("d", [40, 2880, 16384])
+def test_constant_rows(value, d):
+    """A row of one value v has nothing but its bias: what is left of its mean is at most
+    e0 = 146 u |v| in front of the correction and 148 u e0 behind it, times eps^-1/2."""
+    u = 2.0 ** -24
+    X = torch.full((5, d), value, device="cuda")
+    gamma, beta = torch.ones(d, device="cuda"), torch.full((d,), 0.25, device="cuda")
+    Y, mean, rstd = vp.layer_norm(X, gamma, beta, 1e-5)
+    left = 148 * u * 146 * u * abs(value)
+    assert bool(((Y.double() - 0.25).abs() <= left * 1e-5 ** -0.5 * 1.01 + u).all())
+    assert bool(((mean.double() - float(X[0, 0])).abs() <= 1.01 * (u * abs(value) + left)).all())
+    assert bool(((rstd.double() - 1e-5 ** -0.5).abs() <= 1e-5 ** -0.5 * 80 * u).all())
