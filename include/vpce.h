@@ -221,7 +221,8 @@ vp_status vp_ce_check(const void* ws, void* stream, int64_t* bad_targets);
  *   mu_t  = (1/d) sum_j x_tj                        (0 with VP_NORM_RMS)
  *   r_t   = ((1/d) sum_j (x_tj - mu_t)^2 + eps)^(-1/2)
  *   y_tj  = gamma_j (x_tj - mu_t) r_t + beta_j
- * Sums are float32; y is rounded once, to nearest even. */
+ * Sums are float32 (the sum of a row's squares among them: where it leaves float32, as with one
+ * element of 2e19, rstd is 0); y is rounded once, to nearest even. */
 #define VP_NORM_RMS 2u /* no mean: mu_t = 0 in the forward and the backward */
 
 typedef struct {
@@ -229,7 +230,7 @@ typedef struct {
   int64_t d;      /* width, 8..16384 and a multiple of 8 (VP_ERR_SHAPE otherwise) */
   int32_t dtype;  /* vp_dtype of X, gamma, beta and Y */
   uint32_t flags; /* VP_NORM_RMS, VP_ACCUMULATE_DW */
-  double eps;     /* >= 0 and finite (VP_ERR_VALUE otherwise) */
+  double eps;     /* 0, or within float32's normal numbers, 1.2e-38..3.4e38 (VP_ERR_VALUE otherwise) */
 } vp_norm;
 
 /* Workspace of vp_norm_backward in bytes.  Host only. */

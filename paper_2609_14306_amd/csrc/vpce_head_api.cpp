@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "vpce_head.h"
@@ -21,6 +22,8 @@ vp_status validate(const vp_norm* n) {
   if (n->dtype != VP_F32 && n->dtype != VP_BF16) return VP_ERR_DTYPE;
   if (n->T < 0 || n->T > kMaxT || n->d < 8 || n->d % 8 != 0 || n->d > kMaxNormD) return VP_ERR_SHAPE;
   if (!(n->eps >= 0.0) || !std::isfinite(n->eps)) return VP_ERR_VALUE;
+  // (the kernels hold it in float32: no other value may become 0 or infinite there)
+  if (n->eps != 0.0 && (n->eps < FLT_MIN || n->eps > FLT_MAX)) return VP_ERR_VALUE;
   return VP_OK;
 }
 
