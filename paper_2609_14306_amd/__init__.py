@@ -475,7 +475,9 @@ def forward(H, W_shards: List, targets, ignore_index: int = -100, order=None, ws
     With `norm`, H is what the norm takes and its result meets the vocabulary."""
     import torch
     if norm is not None:
-        H = layer_norm(H, norm.gamma, norm.beta, norm.eps, norm.rms)[0]
+        with torch.cuda.device_of(H):  # the norm and the projection on one stream
+            Y = layer_norm(H, norm.gamma, norm.beta, norm.eps, norm.rms)[0]
+            return forward(Y, W_shards, targets, ignore_index, order, ws, strip_elems)
     prob = problem_for(H, W_shards, ignore_index, order, 0, strip_elems)
     fwd_b, _ = vp_ce_workspace_size(prob)
     if ws is None:
@@ -542,11 +544,12 @@ def backward(H, W_shards: List, targets, lse, grad_loss, ignore_index: int = -10
         dgamma, dbeta = (None, None) if dnorm is None else dnorm
         add = accumulate and dnorm is not None
         _check_norm_grads(X, norm.beta is not None, dgamma, dbeta, add)
-        H, mean, rstd = layer_norm(X, norm.gamma, norm.beta, norm.eps, norm.rms)
-        dH, dW_shards = backward(H, W_shards, targets, lse, grad_loss, ignore_index, order, dW_shards,
-                                 accumulate, ws, strip_elems)
-        dH, dgamma, dbeta = layer_norm_backward(X, norm.gamma, mean, rstd, dH, norm.beta is not None, dH,
-                                                dgamma, dbeta, add)
+        with torch.cuda.device_of(X):
+            H, mean, rstd = layer_norm(X, norm.gamma, norm.beta, norm.eps, norm.rms)
+            dH, dW_shards = backward(H, W_shards, targets, lse, grad_loss, ignore_index, order, dW_shards,
+                                     accumulate, ws, strip_elems)
+            dH, dgamma, dbeta = layer_norm_backward(X, norm.gamma, mean, rstd, dH, norm.beta is not None, dH,
+                                                    dgamma, dbeta, add)
         return dH, dW_shards, dgamma, dbeta
     flags = VP_ACCUMULATE_DW if accumulate else 0
     prob = problem_for(H, W_shards, ignore_index, order, flags, strip_elems)

@@ -1,5 +1,5 @@
-"""`backward` with a norm refuses wrong buffers for the norm's gradients on the host, in front of
-the projection (no GPU)."""
+"""`forward` and `backward` with a norm on the host (no GPU): wrong buffers for the norm's gradients
+are refused in front of the projection, and both parts run on the device of the hidden states."""
 import os
 
 import pytest
@@ -55,3 +55,37 @@ def test_dnorm_without_a_norm_is_refused():
     with pytest.raises(ValueError, match="dnorm"):
         vp.backward(torch.zeros(T, D), [torch.zeros(V, D)], torch.zeros(T, dtype=torch.int64), torch.zeros(T),
                     torch.zeros(T), dnorm=(torch.zeros(D), torch.zeros(D)))
+
+
+def test_norm_and_projection_run_on_one_device(monkeypatch):
+    """The norm takes the stream of its tensors' device and the projection the current one: both
+    calls are made with the hidden states' device as the current one."""
+    current, seen = [None], []
+
+    class Device:
+        def __init__(self, t):
+            self.t = t
+
+        def __enter__(self):
+            current[0] = self.t
+
+        def __exit__(self, *_):
+            current[0] = None
+
+    def record(name):
+        return lambda *a, **kw: seen.append((name, current[0] is x))
+
+    x, v = torch.zeros(T, D), torch.zeros(D)
+    W, t = [torch.zeros(V, D)], torch.zeros(T, dtype=torch.int64)
+    monkeypatch.setattr(torch.cuda, "device_of", Device)
+    monkeypatch.setattr(vp.head, "vp_norm_forward", record("norm"))
+    monkeypatch.setattr(vp.head, "vp_norm_backward", record("norm backward"))
+    monkeypatch.setattr(vp, "vp_ce_forward", record("projection"))
+    monkeypatch.setattr(vp, "vp_ce_backward", record("projection backward"))
+    norm = vp.HeadNorm(v, v)
+    loss, lse = vp.forward(x, W, t, norm=norm)
+    assert seen == [("norm", True), ("projection", True)]
+    seen.clear()
+    assert len(vp.backward(x, W, t, lse, loss, norm=norm)) == 4
+    assert seen == [("norm", True), ("projection backward", True), ("norm backward", True)]
+    assert current[0] is None
