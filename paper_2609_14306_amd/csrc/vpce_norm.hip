@@ -350,14 +350,18 @@ bool launched_ok() { return hipGetLastError() == hipSuccess; }
 
 // Run f.run<LANES, EL>() for the layout of a row of d elements.
 //
-// Forward: 32 bytes of X a lane (64 for bfloat16 rows of 2049 to 4096 elements).  Fewer
+// Forward: 32 bytes of X a lane (64 for bfloat16 rows of 2049 to 3456 elements).  Fewer
 // bytes a lane leave more of a workgroup to its two sums, more leave fewer loads in
 // flight, and what counts as few differs by type.  GB/s, bfloat16 / float32:
 //   T = 65536, d = 1000: 64 x 16 5520 / 5020, 128 x 8 4720 / 5630
 //   T = 30000, d = 2048: 128 x 16 5430 / 5610, 256 x 8 4710 / 5860
-//   T = 32768, d = 2880: 128 x 32 5460 / 5480, 256 x 16 5150 / 5870, 512 x 8 4050 / 6010
-//   T = 16384, d = 4096: 128 x 32 5330 / 5370, 256 x 16 5540 / 5730, 512 x 8 4860 / 5950
+//   T = 32768, d = 2880: 128 x 32 5480 / 5480, 256 x 16 5270 / 5870, 512 x 8 4050 / 6010
+//   T = 32768, d = 3456: 128 x 32 5380, 256 x 16 5340 (bfloat16; without a mean 5720, 5830)
+//   T = 16384, d = 3584: 128 x 32 4990, 256 x 16 5220 (bfloat16)
+//   T = 16384, d = 4096: 128 x 32 5320 / 5370, 256 x 16 5530 / 5730, 512 x 8 4860 / 5950
 //   T = 16384, d = 7168: 256 x 32 5240 / 5480, 512 x 16 5330 / 5790, 1024 x 8 4440 / 5880
+// With few rows fewer bytes a lane win (bfloat16, d = 4096, 128 x 32 and 256 x 16: T = 1 3.2 and
+// 2.7 us, T = 512 4.3 and 3.8; T = 4096, which the cache holds, 12.6 and 13.5).
 template <class E, class F>
 bool forward_layout(int d, F&& f) {
   if (d <= 64) return f.template run<8, 8>();
@@ -367,7 +371,8 @@ bool forward_layout(int d, F&& f) {
   if constexpr (E::VEC == 8) {
     if (d <= 1024) return f.template run<64, 16>();
     if (d <= 2048) return f.template run<128, 16>();
-    if (d <= 4096) return f.template run<128, 32>();
+    if (d <= 3456) return f.template run<128, 32>();
+    if (d <= 4096) return f.template run<256, 16>();
     if (d <= 8192) return f.template run<512, 16>();
   } else {
     if (d <= 1024) return f.template run<128, 8>();

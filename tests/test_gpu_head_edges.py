@@ -7,6 +7,7 @@ import torch
 
 import head_plain as hp
 import paper_2609_14306_amd as vp
+import test_gpu_norm as norms
 
 pytestmark = pytest.mark.gpu
 
@@ -139,3 +140,10 @@ def test_constant_rows(value, d):
     assert bool(((Y.double() - 0.25).abs() <= left * 1e-5 ** -0.5 * 1.01 + u).all())
     assert bool(((mean.double() - float(X[0, 0])).abs() <= 1.01 * (u * abs(value) + left)).all())
     assert bool(((rstd.double() - 1e-5 ** -0.5).abs() <= 1e-5 ** -0.5 * 80 * u).all())
+
+
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("d", [2056, 3448, 3456, 3464, 4088, 4096, 4104])
+def test_widths_around_the_layouts_of_bfloat16(d, rms):
+    X, gamma, beta, _ = norms._make(37, d, torch.bfloat16)
+    norms._check_forward(X, gamma, beta, 1e-5, rms, vp.layer_norm(X, gamma, beta, 1e-5, rms))
