@@ -102,8 +102,20 @@ struct Window {
       s += __popcll(__ballot(o <= first));
       for (uint64_t m = __ballot(o > first && o <= last); m; m &= m - 1)
         s += __builtin_amdgcn_readlane(o, __builtin_ctzll(m)) <= t;
-      if (__builtin_amdgcn_readlane(o, 63) > last) return s;
+      const int v = __builtin_amdgcn_readlane(o, 63);
+      if (v > last) return s;
       base += 64;
+      // A window of one offset: a run of empty sequences.  It is left by the largest step of
+      // 64, 128, 256, ... that stays in it (4 M of them inside 64 tokens, a call: 0.2 ms instead
+      // of the 199 of a window at a time).
+      if (__builtin_amdgcn_readlane(o, 0) == v) {
+        const int i = base + (64 << min(lane_id(), 16));
+        const int c = __popcll(__ballot(i <= q.S && q.start[min(i, q.S)] <= v));
+        if (c > 0) {
+          base += 32 << c;
+          s = t < v ? s : base - 1;
+        }
+      }
       load(q);
     }
   }

@@ -4,6 +4,7 @@
 //   ordered     outputs against plain loops in double, for layouts of every kind
 //   disordered  offsets that decrease or leave the tokens: NaN for the sequences that they bound,
 //               every gradient written, nothing outside the arrays touched
+//   runs        long runs of empty sequences, in order and not
 //   no tokens   empty sequences alone, more of them than one workgroup takes among them
 #include <sys/mman.h>
 
@@ -270,6 +271,30 @@ static bool longer() {
   return true;
 }
 
+// Runs of empty sequences longer than a window of offsets, between any two tokens, also where the
+// offsets behind a run go back.
+static bool runs() {
+  std::mt19937_64 rng(8);
+  unsigned seed = 0;
+  for (int T : {3, 130, 2500})
+    for (int S : {64, 130, 1000, 2300})
+      for (int wrong = 0; wrong < 2; ++wrong) {
+        snprintf(what, sizeof what, "runs, T %d S %d seed %u", T, S, seed);
+        std::vector<int> v(S + 1);
+        int at = (int)(rng() % 3);
+        for (int i = 0; i <= S;) {
+          for (int n = 1 + (int)(rng() % 300); n > 0 && i <= S; --n) v[i++] = min(at, T);
+          at += 1 + (int)(rng() % (1 + T / 8));
+        }
+        if (wrong)
+          for (int k = 0; k < 4; ++k) v[rng() % v.size()] = (int)(rng() % (T + 1));
+        at_end = seed % 2 == 0;
+        const Options o = {(seed & 1) != 0, (seed & 2) == 0, (seed & 4) == 0, (seed & 8) != 0, (int)(seed / 2 % 2)};
+        if (!run(T, v, o, seed++)) return false;
+      }
+  return true;
+}
+
 // Sequences without any tokens, from a few to more than one workgroup takes.
 static bool no_tokens() {
   unsigned seed = 0;
@@ -289,6 +314,7 @@ int main(int argc, char** argv) {
                                : !strcmp(argv[1], "disordered") ? all(true)
                                : !strcmp(argv[1], "longer")     ? longer()
                                : !strcmp(argv[1], "no tokens")  ? no_tokens()
+                               : !strcmp(argv[1], "runs")       ? runs()
                                                                 : false);
   printf("%s, %ld launches\n", ok ? "ok" : "FAILED", cpu::launches);
   return ok ? 0 : 1;

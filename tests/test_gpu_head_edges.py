@@ -147,3 +147,28 @@ def test_constant_rows(value, d):
 def test_widths_around_the_layouts_of_bfloat16(d, rms):
     X, gamma, beta, _ = norms._make(37, d, torch.bfloat16)
     norms._check_forward(X, gamma, beta, 1e-5, rms, vp.layer_norm(X, gamma, beta, 1e-5, rms))
+
+
+@pytest.mark.parametrize("T, S", [(128, 2 ** 22), (700, 2 ** 20), (70000, 300000)])
+def test_long_runs_of_empty_sequences(T, S):
+    """Sequences of tokens with up to millions of empty ones between them: sums of whole numbers,
+    exact, and the gradient of each token's own sequence."""
+    g = torch.Generator().manual_seed(S)
+    where = torch.randint(0, T + 1, (40,), generator=g).sort().values  # the offsets that there are
+    start = where[torch.randint(0, 40, (S + 1,), generator=g).sort().values].int()
+    start[0], start[-1] = 0, T
+    loss = torch.randint(0, 64, (T,), generator=g).float()
+    targets = torch.where(torch.rand(T, generator=g) < 0.3, -100, 5)
+    seq = torch.searchsorted(start.long(), torch.arange(T), right=True) - 1
+    keep, up = targets != -100, torch.randint(1, 100, (S,), generator=g).float()
+    adv = torch.randint(-3, 4, (S,), generator=g).float()
+    dev = [v.cuda() for v in (loss, targets, start)]
+    out = vp.policy_forward(*dev, vp.Policy(), adv.cuda())
+    n = torch.zeros(S).index_add_(0, seq[keep], torch.ones(int(keep.sum())))
+    assert torch.equal(out[3].cpu(), n.int()) and torch.equal(out[0].cpu(), -adv * n)
+    grad = vp.policy_backward(*dev, vp.Policy(), adv.cuda(), out[3], up.cuda())
+    assert torch.equal(grad.cpu(), torch.where(keep, up[seq] * adv[seq], torch.zeros(T)))
+    if S % 2 == 0:
+        _, reward, coef = vp.preference_forward(*dev, vp.Preference(beta=1.0))
+        total = torch.zeros(S).index_add_(0, seq[keep], loss[keep])
+        assert torch.equal(reward.cpu(), -total)

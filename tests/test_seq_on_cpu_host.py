@@ -25,7 +25,7 @@ def seq_on_cpu(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("mode", ["ordered", "disordered", "longer", "no tokens"])
+@pytest.mark.parametrize("mode", ["ordered", "disordered", "longer", "no tokens", "runs"])
 def test_kernels_on_the_cpu(seq_on_cpu, mode):
     out = subprocess.run([seq_on_cpu, mode], stdout=subprocess.PIPE, text=True, timeout=240)
     assert out.returncode == 0, out.stdout
