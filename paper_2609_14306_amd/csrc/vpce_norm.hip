@@ -12,9 +12,9 @@
 // the distances.  The backward has the mean in float32 alone: one rounding of it is what xh of
 // such a row is off by there.
 //
-// MI355X, kernels alone: T = 32768, d = 2880, bfloat16 forward 67.9 us (5.6 TB/s), backward
-// 167 + 4.2 us (5.5 TB/s); T = 16384, d = 7168, float32 without a mean 159 us (5.9 TB/s) and
-// 254 + 4.1 us (5.5 TB/s); a 1 GiB copy runs at 5.1 to 5.2 TB/s.
+// MI355X, kernels alone, averages: T = 32768, d = 2880, bfloat16 forward 74 us (5.1 TB/s; 69.2
+// among others of its kind), backward 172 + 4.8 us (5.5 TB/s); T = 16384, d = 7168, float32
+// without a mean 165 us (5.7 TB/s) and 263 + 4.8 us (5.4 TB/s); a 1 GiB copy runs at 5.1 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -8,10 +8,10 @@
 // Bound: up to some 100000 tokens by launches and by the latency of a few dependent loads
 // (offsets, a sequence's values, partial sums); beyond by memory, 16 to 24 bytes a token in
 // the forward and 12 to 28 in the backward, and in the policy forward as much by its float64
-// arithmetic (174 vector instructions for 64 tokens).  MI355X, kernels alone: T = 32768 in 64
-// sequences, policy 4.6 + 1.9 us forward, 3.6 us backward; T = 4.2 M in 4096, 28.3 + 4.0 us
-// (3.6 TB/s) and 21.4 us (5.5 TB/s); preference, T = 4.0 M in 2500 pairs, 14.9 + 3.9 us
-// (4.3 TB/s) and 9.3 us (5.2 TB/s).
+// arithmetic (171 vector instructions for 64 tokens).  MI355X, kernels alone, averages: T = 32768
+// in 64 sequences, policy 4.9 + 2.9 us forward, 3.8 us backward; T = 4.2 M in 4096, 29.6 + 4.7 us
+// (3.4 TB/s) and 22.8 us (5.1 TB/s); preference, T = 4.0 M in 2500 pairs, 16.1 + 4.1 us
+// (4.0 TB/s) and 11.1 us (4.3 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -462,8 +462,8 @@ __global__ void __launch_bounds__(1024) small_kernel(Args args) {
 }
 
 // Gradients: J tokens a lane, one where more would not fill the chip (4 M tokens, J = 1 / 2 /
-// 4: preference 15.2 / 11.4 / 9.1 us, policy 23.2 / 22.4 / 21.5 us; 32768 tokens, policy 3.4 /
-// 4.6 / 6.4 us).
+// 4: preference 16.8 / 12.2 / 10.8 us, policy 24.8 / 24.3 / 22.6 us; 32768 tokens, policy 3.8 /
+// 4.5 / 6.1 us).
 struct PrefGrad {
   SeqArgs q;
   const float* coef;
@@ -559,7 +559,7 @@ bool forward(const Args& a, hipStream_t s) {
     if (!launched_ok()) return false;
   }
   // a unit's parts side by side: a workgroup where there are many (one pair of 131071 tokens:
-  // 4.0 us instead of 5.5 in a wavefront), eight lanes where there are more units than
+  // 4.5 us instead of 5.9 in a wavefront), eight lanes where there are more units than
   // wavefronts
   if (p.chunks >= 512 * (int64_t)units)
     launch_finish<Op, Args, 256>(a, units, s);
