@@ -54,7 +54,7 @@ typedef enum {
   VP_ERR_SHAPE = 2,       /* T out of [0, 2^23 - 256], d out of [8, 2^22] or d % 8 != 0,
                              P out of [1, VP_MAX_SHARDS], V_p out of [0, 2^30], sum V_p out of
                              [1, 2^31 - 1], strip_elems out of [0, 2^30] */
-  VP_ERR_DTYPE = 3,       /* dtype is not VP_F32 / VP_BF16 */
+  VP_ERR_DTYPE = 3,       /* dtype is not VP_F32 / VP_BF16 (or, in the 8-bit calls, not theirs) */
   VP_ERR_ORDER = 4,       /* order is not a permutation of 0..P-1 */
   VP_ERR_ALIGN = 5,       /* a device pointer is not 16-byte aligned (4 for a fold state) */
   VP_ERR_WORKSPACE = 6,   /* workspace pointer NULL or smaller than the size the library asked for */
@@ -66,8 +66,10 @@ typedef enum {
 
 typedef enum {
   VP_F32 = 0,  /* H and W in float32; logits, residual and gradients in float32 */
-  VP_BF16 = 1  /* H and W in bfloat16; products accumulated in float32; the residual
+  VP_BF16 = 1, /* H and W in bfloat16; products accumulated in float32; the residual
                   staged as bfloat16 (round to nearest even); gradients in float32 */
+  VP_E4M3 = 2  /* 8-bit floating point with 4 exponent and 3 mantissa bits (largest value 448,
+                  no infinities) and block scales: vp_score_forward_f8 alone */
 } vp_dtype;
 
 /* flags */
@@ -216,6 +218,82 @@ vp_status vp_ce_plan_info(const vp_problem* prob, vp_plan_info* info);
 vp_status vp_ce_check(const void* ws, void* stream, int64_t* bad_targets);
 
 /* ------------------------------------------------------------------------------
+ * Scoring: what else a token's distribution p_tv = exp(y_tv - lse[t]) says.
+ *   lse, loss   as of vp_ce_forward
+ *   entropy[t]  = - sum_v p_tv log p_tv = lse[t] - sum_v p_tv y_tv
+ *   top_ids[t]  the `top` ids with the largest logits, largest first, the lower id first
+ *               among equal ones, with top_loss[t][k] = lse[t] - y_{t, top_ids[t][k]}
+ *               (= -log p, as loss)
+ * Every token gets its entropy and its ids, also one whose target is ignore_index or out of
+ * range (a serving loop that has no target gives ignore_index).  Logits of minus infinity (masked
+ * vocabulary rows) are the last ids and have top_loss +infinity.  With fewer than `top` ids in the
+ * vocabulary the rest are -1 with top_loss +infinity.  Where lse is not finite (a NaN or plus
+ * infinity among the logits, or none above minus infinity), entropy and top_loss are NaN and
+ * the ids -1.
+ * The order is that of the exact logits: those of all candidates are taken again in float64.
+ * (Candidates come from float32 logits, some more than asked for: more than four groups of
+ * four ids within a rounding of each other can hide one.) */
+#define VP_MAX_TOP 32
+typedef struct {
+  int32_t top; /* alternatives of every token, 0..VP_MAX_TOP (VP_ERR_VALUE otherwise) */
+} vp_score;
+
+/* Workspace of vp_score_forward and vp_score_forward_f8 in bytes.  Host only.  Without
+ * alternatives it does not depend on V; with them it holds maxima of the logits of a chunk
+ * of tokens, at most 1 GiB of them or those of 256 tokens (1.25 bytes for each of a chunk's
+ * logits), and V is at most 2^24 (VP_ERR_SHAPE otherwise). */
+vp_status vp_score_workspace_size(const vp_problem* prob, const vp_score* score, size_t* bytes);
+
+/* H, W_shards, targets, loss, lse as for vp_ce_forward; entropy: device float32 [T], may be NULL;
+ * top_ids: device int64 [T, top] and top_loss: device float32 [T, top], unused without
+ * alternatives.  prob->order is checked and not used.  ws as for vp_ce_forward (vp_ce_check
+ * reads its count of out-of-range targets). */
+vp_status vp_score_forward(const vp_problem* prob, const vp_score* score, const void* H,
+                           const void* const* W_shards, const int64_t* targets, float* loss,
+                           float* lse, float* entropy, int64_t* top_ids, float* top_loss, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* The same for 8-bit operands: prob->dtype is VP_E4M3 (VP_ERR_DTYPE otherwise), d is 16..14336
+ * and a multiple of 16.  Element (t, k) of H stands for its value times 2^(b - 127) with b =
+ * H_scale[t][k / 128]; element (r, k) of W_p for its value times 2^(b - 127) with b =
+ * W_scales[p][r / 128][k / 128] (b = 255 stands for NaN).  H_scale: device uint8 [T, nb],
+ * nb = ceil(d / 128); W_scales: host array of P device pointers, each uint8
+ * [ceil(V_p / 128), nb].  vp_f8_quantize and vp_add_norm_forward make such operands. */
+vp_status vp_score_forward_f8(const vp_problem* prob, const vp_score* score, const void* H,
+                              const uint8_t* H_scale, const void* const* W_shards,
+                              const uint8_t* const* W_scales, const int64_t* targets, float* loss,
+                              float* lse, float* entropy, int64_t* top_ids, float* top_loss, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/* vp_ce_backward of a loss that the entropies enter, too:
+ *   G[t, v] = grad_loss[t] * (p_tv - [v == targets[t]])     0 on ignored tokens
+ *             - grad_entropy[t] * p_tv * (log p_tv + entropy[t])
+ * NaN on out-of-range targets.  An ignored token keeps the second term.  lse, entropy: from
+ * vp_score_forward on the same inputs; grad_loss, grad_entropy: device float32 [T], the upstream
+ * gradients of each token's loss and entropy.  Workspace: vp_ce_workspace_size's of the
+ * backward; everything else as for vp_ce_backward. */
+vp_status vp_score_backward(const vp_problem* prob, const void* H, const void* const* W_shards,
+                            const int64_t* targets, const float* lse, const float* entropy,
+                            const float* grad_loss, const float* grad_entropy, float* dH,
+                            float* const* dW_shards, void* ws, size_t ws_bytes, void* stream);
+
+/* 8-bit values and scales of X [rows, cols], block by block: blocks are 1 x 128 or 128 x 128
+ * elements, fewer at the ends.  A block whose largest finite magnitude is m > 0 has the scale
+ * 2^(b - 127) with the smallest b >= 0 for which m <= 448 * 2^(b - 127) (127 if m is 0 or nothing is
+ * finite); its values are X over the scale to the nearest, ties to even, NaN for NaN and
+ * infinities. */
+typedef struct {
+  int64_t rows;           /* 0..2^30 (VP_ERR_SHAPE otherwise, as for the rest) */
+  int64_t cols;           /* 16..2^22 and a multiple of 16 */
+  int32_t dtype;          /* vp_dtype of X: VP_F32 or VP_BF16 */
+  int32_t rows_per_scale; /* 1 or 128 (VP_ERR_VALUE otherwise) */
+} vp_quant;
+
+/* X: device [rows, cols] of dtype, 16-byte aligned; X8: device [rows, cols] bytes, 16-byte
+ * aligned, no part of X; scale: device uint8 [ceil(rows / rows_per_scale), ceil(cols / 128)]. */
+vp_status vp_f8_quantize(const vp_quant* quant, const void* X, void* X8, uint8_t* scale, void* stream);
+
+/* ------------------------------------------------------------------------------
  * Layer norm of the hidden states, in front of the projection (H of vp_ce_forward is
  * its Y; its dY is the dH of vp_ce_backward):
  *   mu_t  = (1/d) sum_j x_tj                        (0 with VP_NORM_RMS)
@@ -255,6 +333,27 @@ vp_status vp_norm_forward(const vp_norm* norm, const void* X, const void* gamma,
 vp_status vp_norm_backward(const vp_norm* norm, const void* X, const void* gamma, const float* mean,
                            const float* rstd, const float* dY, float* dX, float* dgamma,
                            float* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/* The norm with the residual's addition in front of it and, if wanted, its result in 8 bits:
+ *   S = X + R, rounded to dtype; mu, rstd and y as above, of S's rows as stored
+ * and Y (y rounded) or Y8 and scale (y, held in float32, as vp_f8_quantize holds it in blocks of 1 x
+ * 128), or both.  X, R: device [T, d] of dtype; S: device [T, d] of dtype, may be X or R itself
+ * (no other overlap); Y may be NULL, and so may Y8 and scale together, but not all three
+ * (VP_ERR_NULL).  Y8: device [T, d] bytes, 16-byte aligned; scale: device uint8 [T, ceil(d / 128)];
+ * the rest as for vp_norm_forward, and 16-byte aligned like there. */
+vp_status vp_add_norm_forward(const vp_norm* norm, const void* X, const void* R, const void* gamma,
+                              const void* beta, void* S, void* Y, void* Y8, uint8_t* scale,
+                              float* mean, float* rstd, void* stream);
+
+/* vp_norm_backward at S with the gradient that S has elsewhere added:
+ *   dx_tj = (as of vp_norm_backward) + ds_tj
+ * which is the gradient of X and that of R.  dS: device float32 [T, d], 16-byte aligned, may be NULL
+ * (none); dX may be dY or dS itself.  (Through Y8 the gradient is that of y.)  Workspace:
+ * vp_norm_workspace_size. */
+vp_status vp_add_norm_backward(const vp_norm* norm, const void* S, const void* gamma,
+                               const float* mean, const float* rstd, const float* dY,
+                               const float* dS, float* dX, float* dgamma, float* dbeta, void* ws,
+                               size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------
  * Losses of whole sequences, behind the projection.  They read the per-token loss of

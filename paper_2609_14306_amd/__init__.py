@@ -15,6 +15,11 @@ front of it (``vp_norm_*``, ``layer_norm``; ``forward`` and ``backward`` take on
 ``norm=``), and behind it a preference loss (``vp_pref_*``, ``preference_forward`` /
 ``_backward``) and a clipped policy loss (``vp_policy_*``, ``policy_forward`` /
 ``_backward``) of whole sequences, between the per-token loss and its gradient.
+
+``scoring`` binds the calls that say more of a token's distribution: its entropy and most likely ids
+(``vp_score_*``, ``score``, ``score_f8`` of 8-bit operands), the gradients with an entropy term
+(``backward`` takes it as ``grad_entropy=``), and the 8-bit operands (``vp_f8_quantize``, ``quantize``;
+``add_norm`` makes them of a norm's rows).
 """
 from __future__ import annotations
 
@@ -28,10 +33,11 @@ LIB_PATH = os.path.join(_PKG, "libvpce.so")
 VP_OK, VP_ERR_NULL, VP_ERR_SHAPE, VP_ERR_DTYPE, VP_ERR_ORDER = 0, 1, 2, 3, 4
 VP_ERR_ALIGN, VP_ERR_WORKSPACE, VP_ERR_TARGET, VP_ERR_HIP, VP_ERR_UNSUPPORTED = 5, 6, 7, 8, 9
 VP_ERR_VALUE = 10
-VP_F32, VP_BF16 = 0, 1
+VP_F32, VP_BF16, VP_E4M3 = 0, 1, 2
 VP_ACCUMULATE_DW, VP_NORM_RMS, VP_SEQ_MEAN, VP_ADV_PER_TOKEN = 1, 2, 4, 8
 VP_PREF_LOGISTIC, VP_PREF_SQUARED = 0, 1
 VP_MAX_SHARDS = 64
+VP_MAX_TOP = 32
 
 EXPORTED = ("vp_ce_workspace_size", "vp_ce_forward", "vp_ce_forward_noalloc", "vp_ce_backward",
             "vp_ce_state_init",
@@ -39,6 +45,8 @@ EXPORTED = ("vp_ce_workspace_size", "vp_ce_forward", "vp_ce_forward_noalloc", "v
             "vp_norm_workspace_size", "vp_norm_forward", "vp_norm_backward",
             "vp_seq_workspace_size", "vp_pref_forward", "vp_pref_backward",
             "vp_policy_forward", "vp_policy_backward",
+            "vp_score_workspace_size", "vp_score_forward", "vp_score_forward_f8", "vp_score_backward",
+            "vp_f8_quantize", "vp_add_norm_forward", "vp_add_norm_backward",
             "vp_status_str", "vp_abi_version")
 
 
@@ -85,6 +93,15 @@ class vp_preference(ctypes.Structure):
 class vp_policy(ctypes.Structure):
     _fields_ = [("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_coef", ctypes.c_double),
                 ("flags", ctypes.c_uint32)]
+
+
+class vp_score(ctypes.Structure):
+    _fields_ = [("top", ctypes.c_int32)]
+
+
+class vp_quant(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("rows_per_scale", ctypes.c_int32)]
 
 
 _lib = None
@@ -134,7 +151,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                      (lib.vp_pref_forward, [P(vp_sequences), P(vp_preference)] + [vptr] * 8 + [size, vptr]),
                      (lib.vp_pref_backward, [P(vp_sequences)] + [vptr] * 6),
                      (lib.vp_policy_forward, [P(vp_sequences), P(vp_policy)] + [vptr] * 11 + [size, vptr]),
-                     (lib.vp_policy_backward, [P(vp_sequences), P(vp_policy)] + [vptr] * 10)):
+                     (lib.vp_policy_backward, [P(vp_sequences), P(vp_policy)] + [vptr] * 10),
+                     (lib.vp_score_workspace_size, [vp, P(vp_score), P(size)]),
+                     (lib.vp_score_forward, [vp, P(vp_score), vptr, P(vptr)] + [vptr] * 7 + [size, vptr]),
+                     (lib.vp_score_forward_f8, [vp, P(vp_score), vptr, vptr, P(vptr), P(vptr)] + [vptr] * 7 +
+                      [size, vptr]),
+                     (lib.vp_score_backward, [vp, vptr, P(vptr)] + [vptr] * 6 + [P(vptr), vptr, size, vptr]),
+                     (lib.vp_f8_quantize, [P(vp_quant)] + [vptr] * 4),
+                     (lib.vp_add_norm_forward, [P(vp_norm)] + [vptr] * 11),
+                     (lib.vp_add_norm_backward, [P(vp_norm)] + [vptr] * 10 + [size, vptr])):
         fn.restype = ctypes.c_int
         fn.argtypes = args
     _lib = lib
@@ -195,6 +220,8 @@ def _check(status: int, what: str) -> None:
 # checked first and the device last, so that every refusal is raised on the host.
 def _torch_dtype(code: int):
     import torch
+    if code == VP_E4M3:
+        return torch.float8_e4m3fn
     return torch.bfloat16 if code == VP_BF16 else torch.float32
 
 
@@ -455,9 +482,10 @@ def _dtype_code(t) -> int:
     raise TypeError(f"unsupported dtype {t.dtype} (bfloat16 or float32)")
 
 
-from .head import (HeadNorm, Norm, Policy, Preference, Sequences, layer_norm,  # noqa: E402
-                   layer_norm_backward, policy_backward, policy_forward, preference_backward,
-                   preference_forward, vp_norm_backward, vp_norm_forward, vp_norm_workspace_size,
+from .head import (HeadNorm, Norm, Policy, Preference, Sequences, add_norm, add_norm_backward,  # noqa: E402
+                   layer_norm, layer_norm_backward, policy_backward, policy_forward, preference_backward,
+                   preference_forward, vp_add_norm_backward, vp_add_norm_forward, vp_norm_backward,
+                   vp_norm_forward, vp_norm_workspace_size,
                    vp_policy_backward, vp_policy_forward, vp_pref_backward, vp_pref_forward,
                    vp_seq_workspace_size, _check_norm_grads)
 
@@ -466,6 +494,10 @@ def problem_for(H, W_shards, ignore_index: int = -100, order=None, flags: int = 
                 strip_elems: int = 0) -> Problem:
     return Problem(H.shape[0], H.shape[1], [w.shape[0] for w in W_shards], _dtype_code(H), order,
                    ignore_index, flags, strip_elems)
+
+
+from .scoring import (Quant, Score, f8_buffers, quantize, score, score_f8, vp_f8_quantize,  # noqa: E402
+                    vp_score_backward, vp_score_forward, vp_score_forward_f8, vp_score_workspace_size)
 
 
 def forward(H, W_shards: List, targets, ignore_index: int = -100, order=None, ws=None,
@@ -529,8 +561,12 @@ def fold_finalize(targets, state, shard_rows: Sequence[int], ignore_index: int =
 
 def backward(H, W_shards: List, targets, lse, grad_loss, ignore_index: int = -100, order=None,
              dW_shards=None, accumulate: bool = False, ws=None, strip_elems: int = 0,
-             norm: Optional[HeadNorm] = None, dnorm=None):
+             norm: Optional[HeadNorm] = None, dnorm=None, entropy=None, grad_entropy=None):
     """(dH [T, d], [dW_p [V_p, d]]) float32, recomputing the logits from the saved lse.
+
+    With `grad_entropy` [T], the upstream gradient of each token's entropy, and `entropy` [T] (both
+    from ``score``, which gives the same loss and lse as ``forward``), the gradients of a loss with an
+    entropy term.
 
     With `norm` (as given to `forward`): (dH, [dW_p], dgamma, dbeta) with the gradient of the
     norm's input as dH, written over that of its result; the norm is recomputed.  dbeta is None
@@ -539,6 +575,8 @@ def backward(H, W_shards: List, targets, lse, grad_loss, ignore_index: int = -10
     import torch
     if norm is None and dnorm is not None:
         raise ValueError("dnorm: there is no norm that it is of")
+    if (entropy is None) != (grad_entropy is None):
+        raise ValueError("entropy and grad_entropy: one of them is missing")
     if norm is not None:
         X = H
         dgamma, dbeta = (None, None) if dnorm is None else dnorm
@@ -547,7 +585,7 @@ def backward(H, W_shards: List, targets, lse, grad_loss, ignore_index: int = -10
         with torch.cuda.device_of(X):
             H, mean, rstd = layer_norm(X, norm.gamma, norm.beta, norm.eps, norm.rms)
             dH, dW_shards = backward(H, W_shards, targets, lse, grad_loss, ignore_index, order, dW_shards,
-                                     accumulate, ws, strip_elems)
+                                     accumulate, ws, strip_elems, entropy=entropy, grad_entropy=grad_entropy)
             dH, dgamma, dbeta = layer_norm_backward(X, norm.gamma, mean, rstd, dH, norm.beta is not None, dH,
                                                     dgamma, dbeta, add)
         return dH, dW_shards, dgamma, dbeta
@@ -560,5 +598,8 @@ def backward(H, W_shards: List, targets, lse, grad_loss, ignore_index: int = -10
     if dW_shards is None:
         dW_shards = [torch.empty(w.shape[0], prob.d, dtype=torch.float32, device=H.device)
                      for w in W_shards]
-    vp_ce_backward(prob, H, W_shards, targets, lse, grad_loss, dH, dW_shards, ws)
+    if grad_entropy is not None:
+        vp_score_backward(prob, H, W_shards, targets, lse, entropy, grad_loss, grad_entropy, dH, dW_shards, ws)
+    else:
+        vp_ce_backward(prob, H, W_shards, targets, lse, grad_loss, dH, dW_shards, ws)
     return dH, dW_shards

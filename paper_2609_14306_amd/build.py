@@ -14,7 +14,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libvpce.so")
 SOURCES = [os.path.join(CSRC, name) for name in
-           ("vpce_kernels.hip", "vpce_api.cpp", "vpce_norm.hip", "vpce_seq.hip", "vpce_head_api.cpp")]
+           ("vpce_kernels.hip", "vpce_api.cpp", "vpce_norm.hip", "vpce_seq.hip", "vpce_head_api.cpp",
+            "vpce_entropy.hip", "vpce_score.hip", "vpce_f8.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

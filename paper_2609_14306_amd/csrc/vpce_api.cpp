@@ -25,14 +25,15 @@ inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 inline int64_t round_down(int64_t x, int64_t m) { return x / m * m; }
 inline int64_t ceil_div(int64_t x, int64_t m) { return (x + m - 1) / m; }
 
-size_t elem_bytes(int dtype) { return dtype == VP_BF16 ? 2 : 4; }
+size_t elem_bytes(int dtype) { return dtype == VP_E4M3 ? 1 : dtype == VP_BF16 ? 2 : 4; }
 
 constexpr int64_t kMaxT = (1ll << 23) - 256;
 constexpr int64_t kMaxD = 1ll << 22;
 
-vp_status validate(const vp_problem* p, int64_t* V_out, bool allow_empty_vocab = false) {
+vp_status validate(const vp_problem* p, int64_t* V_out, bool allow_empty_vocab = false, bool f8 = false) {
   if (!p) return VP_ERR_NULL;
-  if (p->dtype != VP_F32 && p->dtype != VP_BF16) return VP_ERR_DTYPE;
+  if (f8 ? p->dtype != VP_E4M3 : p->dtype != VP_F32 && p->dtype != VP_BF16) return VP_ERR_DTYPE;
+  if (f8 && (p->d % 16 != 0 || p->d > vpce::kF8MaxD)) return VP_ERR_SHAPE;
   // The bf16 GEMM tiles address a 256-row operand tile with 32-bit byte offsets
   // (256 rows x leading dimension x 2 bytes < 2^32): leading dimensions are d,
   // the padded token count and strip widths, so T and d are capped below 2^23.
@@ -156,6 +157,7 @@ FwdPlan plan_fwd(const vp_problem* p, int64_t slots) {
   }
   double best_time = 0;
   for (int kind = 0; kind < vpce::kFwdKinds; ++kind) {
+    if (kind == 1 && p->dtype == VP_E4M3) continue;  // (not built)
     const vpce::FwdTile t = vpce::fwd_tile(p->dtype, kind);
     const int64_t blocks = ceil_div(p->T, t.bn), places = kCUs * t.per_cu;
     const int64_t tiles = std::max<int64_t>(1, count_tiles(p, t.bm));
@@ -713,10 +715,16 @@ vp_status vp_ce_plan_info(const vp_problem* prob, vp_plan_info* info) {
   return VP_OK;
 }
 
-vp_status vp_ce_backward(const vp_problem* prob, const void* H, const void* const* W_shards,
-                         const int64_t* targets, const float* lse, const float* grad_loss,
-                         float* dH, float* const* dW_shards, void* ws, size_t ws_bytes,
-                         void* stream) {
+}  // extern "C"
+
+namespace {
+
+// The backward; with_entropy: the loss has an entropy term (vp_score_backward).
+vp_status backward_impl(const vp_problem* prob, const void* H, const void* const* W_shards,
+                        const int64_t* targets, const float* lse, const float* entropy,
+                        const float* grad_loss, const float* grad_entropy, bool with_entropy,
+                        float* dH, float* const* dW_shards, void* ws, size_t ws_bytes,
+                        void* stream) {
   int64_t V = 0;
   vp_status st = validate(prob, &V);
   if (st != VP_OK) return st;
@@ -732,6 +740,7 @@ vp_status vp_ce_backward(const vp_problem* prob, const void* H, const void* cons
   const int64_t T = prob->T;
   if (T > 0) {
     if (!H || !targets || !lse || !grad_loss || !dH) return VP_ERR_NULL;
+    if (with_entropy && (!entropy || !grad_entropy)) return VP_ERR_NULL;
     if (misaligned(H) || misaligned(dH)) return VP_ERR_ALIGN;
   }
   hipStream_t s = (hipStream_t)stream;
@@ -823,6 +832,8 @@ vp_status vp_ce_backward(const vp_problem* prob, const void* H, const void* cons
     a.g.ignore_index = prob->ignore_index;
     a.g.yt = yt;
     a.g.d = (int32_t)d;
+    a.entropy = entropy;
+    a.grad_entropy = grad_entropy;
     if (k < n) {
       const BwdStrip& st = f.strips[k / n_tc];
       a.g.t0 = k % n_tc * f.Tc;
@@ -871,6 +882,210 @@ vp_status vp_ce_backward(const vp_problem* prob, const void* H, const void* cons
   }
   if (f.max_jobs > 1 && !vpce::run_sum_parts(part, f.max_jobs, T * d, dH, s)) return VP_ERR_HIP;
   return VP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+vp_status vp_ce_backward(const vp_problem* prob, const void* H, const void* const* W_shards,
+                         const int64_t* targets, const float* lse, const float* grad_loss,
+                         float* dH, float* const* dW_shards, void* ws, size_t ws_bytes,
+                         void* stream) {
+  return backward_impl(prob, H, W_shards, targets, lse, nullptr, grad_loss, nullptr, false, dH, dW_shards, ws,
+                       ws_bytes, stream);
+}
+
+vp_status vp_score_backward(const vp_problem* prob, const void* H, const void* const* W_shards,
+                            const int64_t* targets, const float* lse, const float* entropy,
+                            const float* grad_loss, const float* grad_entropy, float* dH,
+                            float* const* dW_shards, void* ws, size_t ws_bytes, void* stream) {
+  return backward_impl(prob, H, W_shards, targets, lse, entropy, grad_loss, grad_entropy, true, dH, dW_shards, ws,
+                       ws_bytes, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+// Scoring.  Without alternatives it is one forward over all tokens.  With them the maxima of the
+// logits (1 to 1.25 bytes for each logit, see vpce::ScoreArgs) wait in the workspace for the tokens'
+// workgroups, so the tokens go through in chunks whose maxima take at most kTopBytes, or of 256.
+constexpr int64_t kTopBytes = 1ll << 30;
+constexpr int64_t kMaxTopV = 1ll << 24;
+
+struct ScorePlan {
+  int64_t Tc;                  // tokens of a chunk (all chunks but the last)
+  int64_t slots;               // partial states
+  size_t off_m, off_s, off_u, off_fine, off_coarse, total;
+};
+ScorePlan score_plan(const vp_problem* p, int top) {
+  ScorePlan s;
+  int64_t rows = 0;  // of the largest tiles, padding among them
+  for (int q = 0; q < p->P; ++q) rows += round_up(p->shard_rows[q], 256);
+  s.Tc = p->T;
+  if (top > 0) {
+    const int64_t most = std::max<int64_t>(256, round_down(kTopBytes / (rows + rows / 4), 256));
+    if (p->T > most) s.Tc = round_up(ceil_div(p->T, ceil_div(p->T, most)), 256);
+  }
+  vp_problem part = *p;
+  part.T = s.Tc;
+  s.slots = partial_slots(&part);
+  if (s.Tc > 0) {
+    part.T = p->T % s.Tc;
+    s.slots = std::max(s.slots, partial_slots(&part));
+  }
+  const size_t plane = align256((size_t)s.slots * 4);
+  s.off_m = kHeaderBytes;
+  s.off_s = s.off_m + plane;
+  s.off_u = s.off_s + plane;
+  s.off_fine = s.off_u + plane;
+  s.off_coarse = s.off_fine + (top > 0 ? align256((size_t)(s.Tc * rows)) : 0);
+  s.total = s.off_coarse + (top > 0 ? align256((size_t)(s.Tc * (rows / 4))) : 0);
+  return s;
+}
+
+vp_status validate(const vp_problem* p, const vp_score* score, bool f8, int64_t* V) {
+  const vp_status st = validate(p, V, false, f8);
+  if (st != VP_OK) return st;
+  if (!score) return VP_ERR_NULL;
+  if (score->top < 0 || score->top > VP_MAX_TOP) return VP_ERR_VALUE;
+  if (score->top > 0 && *V > kMaxTopV) return VP_ERR_SHAPE;
+  return VP_OK;
+}
+
+vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, const void* H,
+                     const uint8_t* H_scale, const void* const* W_shards,
+                     const uint8_t* const* W_scales, const int64_t* targets, float* loss, float* lse,
+                     float* entropy, int64_t* top_ids, float* top_loss, void* ws, size_t ws_bytes,
+                     hipStream_t s) {
+  int64_t V = 0;
+  vp_status st = validate(prob, score, f8, &V);
+  if (st != VP_OK) return st;
+  if ((st = check_shards(prob, W_shards)) != VP_OK) return st;
+  if (f8) {
+    if (!W_scales) return VP_ERR_NULL;
+    for (int q = 0; q < prob->P; ++q)
+      if (prob->shard_rows[q] > 0 && !W_scales[q]) return VP_ERR_NULL;
+  }
+  const int top = score->top;
+  const ScorePlan plan = score_plan(prob, top);
+  if (!ws || ws_bytes < plan.total) return VP_ERR_WORKSPACE;
+  if (misaligned(ws)) return VP_ERR_ALIGN;
+  if (prob->T > 0) {
+    if (!H || (f8 && !H_scale) || !targets || !loss || !lse || (top > 0 && (!top_ids || !top_loss)))
+      return VP_ERR_NULL;
+    if (misaligned(H)) return VP_ERR_ALIGN;
+  }
+  unsigned long long* counter = (unsigned long long*)ws;
+  if (prob->T == 0) return vpce::run_ws_init(counter, s) ? VP_OK : VP_ERR_HIP;
+
+  vp_problem part = *prob;
+  part.order = nullptr;  // ids in order, so that a lower tile has the lower ids
+  char* base = (char*)ws;
+  for (int64_t t0 = 0; t0 < prob->T; t0 += plan.Tc) {
+    const int64_t T = part.T = std::min(plan.Tc, prob->T - t0);
+    const FwdPlan fp = plan_fwd(&part, plan.slots);
+    const vpce::FwdTile ft = vpce::fwd_tile(prob->dtype, fp.kind);
+    vpce::TopArgs a;
+    memset(&a, 0, sizeof(a));
+    vpce::FwdArgs& f = a.s.f;
+    build_table(&part, W_shards, ft.bm, &f.st, &f.n_tiles);
+    f.H = (const char*)H + (size_t)(t0 * prob->d) * elem_bytes(prob->dtype);
+    f.targets = targets + t0;
+    f.T = T;
+    f.d = (int32_t)prob->d;
+    f.n_tok_blocks = (int32_t)ceil_div(T, ft.bn);
+    f.n_splits = fp.splits;
+    f.kind = fp.kind;
+    f.counter = t0 == 0 ? counter : nullptr;
+    f.m_part = (float*)(base + plan.off_m);
+    f.s_part = (float*)(base + plan.off_s);
+    a.s.u_part = (float*)(base + plan.off_u);
+    if (top > 0) {
+      a.s.fine = (float*)(base + plan.off_fine);
+      a.s.coarse = (float*)(base + plan.off_coarse);
+    }
+    if (f8) {
+      a.s.nb = (int32_t)ceil_div(prob->d, 128);
+      a.s.h_scale = H_scale + t0 * a.s.nb;
+      for (int q = 0; q < prob->P; ++q) a.s.w_scale[q] = W_scales[q];
+    }
+    if (!vpce::run_score(prob->dtype, a.s, s)) return VP_ERR_HIP;
+
+    vpce::ScoreCombArgs c;
+    memset(&c, 0, sizeof(c));
+    c.c.m_part = f.m_part;
+    c.c.s_part = f.s_part;
+    c.c.targets = f.targets;
+    c.c.T = T;
+    c.c.V = V;
+    c.c.ignore_index = prob->ignore_index;
+    c.c.n_splits = fp.splits;
+    c.c.loss = loss + t0;
+    c.c.lse = lse + t0;
+    c.c.bad_counter = counter;
+    c.u_part = a.s.u_part;
+    c.entropy = entropy ? entropy + t0 : nullptr;
+    if (!vpce::run_score_comb(prob->dtype, c, a.s, s)) return VP_ERR_HIP;
+    if (top == 0) continue;
+    a.lse = c.c.lse;
+    a.bm = ft.bm;
+    a.cpt = vpce::score_coarse(fp.kind);
+    a.top = top;
+    a.ids = top_ids + t0 * top;
+    a.loss = top_loss + t0 * top;
+    if (!vpce::run_top(prob->dtype, a, s)) return VP_ERR_HIP;
+  }
+  return VP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+vp_status vp_score_workspace_size(const vp_problem* prob, const vp_score* score, size_t* bytes) {
+  int64_t V = 0;
+  const vp_status st = validate(prob, score, prob && prob->dtype == VP_E4M3, &V);
+  if (st != VP_OK) return st;
+  if (bytes) *bytes = score_plan(prob, score->top).total;
+  return VP_OK;
+}
+
+vp_status vp_score_forward(const vp_problem* prob, const vp_score* score, const void* H,
+                           const void* const* W_shards, const int64_t* targets, float* loss,
+                           float* lse, float* entropy, int64_t* top_ids, float* top_loss, void* ws,
+                           size_t ws_bytes, void* stream) {
+  return score_impl(prob, score, false, H, nullptr, W_shards, nullptr, targets, loss, lse, entropy, top_ids,
+                    top_loss, ws, ws_bytes, (hipStream_t)stream);
+}
+
+vp_status vp_score_forward_f8(const vp_problem* prob, const vp_score* score, const void* H,
+                              const uint8_t* H_scale, const void* const* W_shards,
+                              const uint8_t* const* W_scales, const int64_t* targets, float* loss,
+                              float* lse, float* entropy, int64_t* top_ids, float* top_loss, void* ws,
+                              size_t ws_bytes, void* stream) {
+  return score_impl(prob, score, true, H, H_scale, W_shards, W_scales, targets, loss, lse, entropy, top_ids,
+                    top_loss, ws, ws_bytes, (hipStream_t)stream);
+}
+
+vp_status vp_f8_quantize(const vp_quant* q, const void* X, void* X8, uint8_t* scale, void* stream) {
+  if (!q) return VP_ERR_NULL;
+  if (q->dtype != VP_F32 && q->dtype != VP_BF16) return VP_ERR_DTYPE;
+  if (q->rows < 0 || q->rows > (1ll << 30) || q->cols < 16 || q->cols % 16 != 0 || q->cols > (1ll << 22))
+    return VP_ERR_SHAPE;
+  if (q->rows_per_scale != 1 && q->rows_per_scale != 128) return VP_ERR_VALUE;
+  if (q->rows == 0) return VP_OK;
+  if (!X || !X8 || !scale) return VP_ERR_NULL;
+  if (misaligned(X) || misaligned(X8)) return VP_ERR_ALIGN;
+  vpce::QuantArgs a;
+  a.X = X;
+  a.X8 = (uint8_t*)X8;
+  a.scale = scale;
+  a.rows = q->rows;
+  a.cols = (int32_t)q->cols;
+  a.nb = (int32_t)ceil_div(q->cols, 128);
+  return vpce::run_quantize(q->dtype, a, q->rows_per_scale, (hipStream_t)stream) ? VP_OK : VP_ERR_HIP;
 }
 
 vp_status vp_ce_check(const void* ws, void* stream, int64_t* bad_targets) {

@@ -49,9 +49,17 @@ __device__ __forceinline__ void store_tile_blocked(const uint16_t* lds, uint16_t
 // summation order).  bfloat16 tiles go through LDS (free once the mainloop returns)
 // once per layout, so that both layouts leave as whole 16-byte chunks, 1 KiB per
 // wavefront store; the target elements are patched in LDS before each store.
-template <class E, class G>
-__device__ __forceinline__ void grad_tile(const GradArgs& a, int vt, int tb,
-                                          typename E::storage* smem) {
+//
+// ENT: the loss has an entropy term, with the upstream gradient e of the token's entropy S =
+// lse - sum_v p_v y_v.  dS / dy_v = -p_v (log p_v + S), so
+//   G = g (p - onehot) - e p (log p + S) = p ((g - e S) - e log p) - g onehot,
+// two multiply-adds, an exponential and a product per element with x = log2 p, which is held at
+// kLeastLog2 from below: a logit of minus infinity has p = 0 and would give 0 * infinity.  An
+// ignored token has g = 0 and keeps its entropy's term.
+constexpr float kLeastLog2 = -1e4f;
+template <class E, class G, bool ENT>
+__device__ __forceinline__ void grad_tile(const GradArgs& a, const float* entropy, const float* grad_entropy,
+                                          int vt, int tb, typename E::storage* smem) {
   using S = typename E::storage;
   constexpr int BM = G::BM, BN = G::BN, MB = G::MB, NB = G::NB;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -63,7 +71,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, int vt, int tb,
   // paid after it.  Columns past the chunk read its last token (N >= 1 whenever a
   // residual tile runs) and are masked below.
   int64_t tgv[NB];
-  float gv[NB], lsev[NB], ytv[NB];
+  float gv[NB], lsev[NB], ytv[NB], sv[NB], ev[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
     const int64_t t = a.t0 + min(n0 + wn + 32 * j + (lane & 31), a.N - 1);
@@ -71,6 +79,8 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, int vt, int tb,
     gv[j] = a.grad[t];
     lsev[j] = a.lse[t];
     ytv[j] = a.yt[t];
+    sv[j] = ENT ? entropy[t] : 0.f;
+    ev[j] = ENT ? grad_entropy[t] : 0.f;
   }
 
   f32x16_t acc[MB][NB];
@@ -83,6 +93,9 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, int vt, int tb,
   // it needs, in front of the mainloop)
 #pragma unroll
   for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(tgv[j]), "+v"(gv[j]), "+v"(lsev[j]), "+v"(ytv[j]));
+  if constexpr (ENT)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(sv[j]), "+v"(ev[j]));
 
   // Strip offsets fit in 32 bits (the strip budget is capped below 2^31 elements).
   // Both strips are k-blocked (see GradArgs) with KB = E::KB elements per block.
@@ -101,7 +114,8 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, int vt, int tb,
   const int lim = a.M - m0 - wm - 4 * (lane >> 5);
   // Per token column j of this lane: the exponent offset, the sign of g, and the
   // target element this lane owns (tile row, or -1) with its value.
-  float cexp[NB], vt_val[NB];
+  // (ENT: cexp is -lse log2e, and a residual element p (wg + wx log2 p).)
+  float cexp[NB], vt_val[NB], wg[NB], wx[NB];
   uint32_t sgn[NB];
   int trow[NB];
 #pragma unroll
@@ -110,24 +124,31 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, int vt, int tb,
     cexp[j] = -INFINITY;
     sgn[j] = 0u;
     trow[j] = -1;
-    vt_val[j] = 0.f;
+    vt_val[j] = wg[j] = wx[j] = 0.f;
     if (nl < a.N) {
       const int64_t tg = tgv[j];
+      if (ENT) {
+        cexp[j] = -lsev[j] * kLog2e;
+        wg[j] = -ev[j] * sv[j];
+        wx[j] = -ev[j] * kLn2;
+      }
       if (tg != a.ignore_index) {
         float g = gv[j];
         if (tg < 0 || tg >= a.V) g = __builtin_nanf("");  // out of range: NaN row
         const float lse2 = lsev[j] * kLog2e;
         const float ag = __builtin_fabsf(g);
-        cexp[j] = __builtin_amdgcn_logf(ag) - lse2;  // log2|g| - lse log2e
-        sgn[j] = g < 0.f ? 0x80008000u : 0u;
+        if (!ENT) cexp[j] = __builtin_amdgcn_logf(ag) - lse2;  // log2|g| - lse log2e
+        sgn[j] = !ENT && g < 0.f ? 0x80008000u : 0u;
         // the target element: inside the chunk (its padding rows stay zero), in this
         // wave's rows of the tile and in this lane half
         const int64_t rel = tg - a.gid0 - m0 - wm;
         if (tg - a.gid0 < a.M && rel >= 0 && rel < G::WM && (int)((rel >> 2) & 1) == (lane >> 5)) {
           trow[j] = (int)rel + wm;
-          const float pt = __builtin_amdgcn_exp2f(__builtin_fmaf(ytv[j], kLog2e, -lse2));
+          const float xt = __builtin_fmaf(ytv[j], kLog2e, -lse2), pt = __builtin_amdgcn_exp2f(xt);
           vt_val[j] = g * (pt - 1.f);
+          if (ENT) vt_val[j] = __builtin_fmaf(pt, __builtin_fmaf(wx[j], fmaxf(xt, kLeastLog2), wg[j]), vt_val[j]);
         }
+        if (ENT) wg[j] += g;
       }
     }
   }
@@ -149,7 +170,14 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, int vt, int tb,
         float v4[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r4 + q], kLog2e, cexp[j]));
+          const float x = __builtin_fmaf(acc[i][j][r4 + q], kLog2e, cexp[j]);
+          float e;
+          if constexpr (ENT) {
+            const float xl = fmaxf(x, kLeastLog2);
+            e = __builtin_amdgcn_exp2f(xl) * __builtin_fmaf(wx[j], xl, wg[j]);
+          } else {
+            e = __builtin_amdgcn_exp2f(x);
+          }
           v4[q] = (!MASKED || 32 * i + r4 / 4 * 8 + q < lim) ? e : 0.f;
         }
         if constexpr (kBlocked) {
@@ -377,7 +405,7 @@ __device__ __forceinline__ void contract_tile(const StageArgs& a, bool is_dh, in
 // order[p], numbered from first[p][x], for p = 0, 1, 2: every XCD gets an even share of
 // each kind, consecutive tiles of one kind stay on one XCD's L2, and the longest tiles go
 // first so that the partly filled last round is made of the short ones.
-template <class E, class GL, class GC, class GW>
+template <class E, class GL, class GC, class GW, bool ENT>
 __global__ void __launch_bounds__(GC::NT, GC::OCC* GC::NT / 256) bwd_stage_kernel(StageArgs a, StageSplit sp) {
   static_assert(GL::NT == GC::NT && GL::BN == GC::BN && GL::BM == GC::BM, "one tile shape");
   using S = typename E::storage;
@@ -402,7 +430,7 @@ __global__ void __launch_bounds__(GC::NT, GC::OCC* GC::NT / 256) bwd_stage_kerne
     const int64_t row0 = a.gseg[q].row0;
     g.strip = (S*)g.strip + row0 * E::KB;
     g.strip_t = (S*)g.strip_t + row0 / E::KB * g.Tc * E::KB;
-    grad_tile<E, GL>(g, mt - (int)row0 / GL::BM, nt, smem);
+    grad_tile<E, GL, ENT>(g, a.entropy, a.grad_entropy, mt - (int)row0 / GL::BM, nt, smem);
     return;
   }
   const ColBlocks cb = col_blocks<GC, GW>(a.g.d);
@@ -462,7 +490,7 @@ static StageSplit split_stage(const int n_kind[3]) {
   return sp;
 }
 
-template <class E, class GL, class GC, class GW = GC>
+template <class E, bool ENT, class GL, class GC, class GW = GC>
 static bool launch_stage_g(const StageArgs& a, hipStream_t s) {
   const int n_tb = (a.g.N + GL::BN - 1) / GL::BN, n_cb = (a.c_N + GC::BN - 1) / GC::BN;
   const int n_nb = col_blocks<GC, GW>(a.g.d).n;
@@ -470,23 +498,23 @@ static bool launch_stage_g(const StageArgs& a, hipStream_t s) {
   int n_kind[3], n = 0;
   for (int p = 0; p < 3; ++p) n += n_kind[p] = tiles[a.order[p]];
   if (n == 0) return true;
-  hipLaunchKernelGGL((bwd_stage_kernel<E, GL, GC, GW>), dim3((unsigned)n), dim3(GC::NT), 0, s, a,
+  hipLaunchKernelGGL((bwd_stage_kernel<E, GL, GC, GW, ENT>), dim3((unsigned)n), dim3(GC::NT), 0, s, a,
                      split_stage(n_kind));
   return launched_ok();
 }
-template <class E>
+template <class E, bool ENT>
 static bool launch_stage(int cls, const StageArgs& a, hipStream_t s) {
   using C = Cfg<E>;
-  if (cls == 1) return launch_stage_g<E, typename C::Res128x64, typename C::Tr128x64>(a, s);
-  if (cls == 2) return launch_stage_g<E, typename C::Res128, typename C::Tr128>(a, s);
+  if (cls == 1) return launch_stage_g<E, ENT, typename C::Res128x64, typename C::Tr128x64>(a, s);
+  if (cls == 2) return launch_stage_g<E, ENT, typename C::Res128, typename C::Tr128>(a, s);
   const bool whole = a.g.d % E::KB == 0;
   if constexpr (sizeof(typename E::storage) == 2) {
-    if (cls == 0 && whole) return launch_stage_g<E, typename C::Logits, typename C::Tr256, typename C::Tr320>(a, s);
-    if (cls == 0) return launch_stage_g<E, typename C::LogitsTail, typename C::Tr256, typename C::Tr320>(a, s);
+    if (cls == 0 && whole) return launch_stage_g<E, ENT, typename C::Logits, typename C::Tr256, typename C::Tr320>(a, s);
+    if (cls == 0) return launch_stage_g<E, ENT, typename C::LogitsTail, typename C::Tr256, typename C::Tr320>(a, s);
   }
   if (cls != 3) return false;
-  if (whole) return launch_stage_g<E, typename C::Logits, typename C::Mm, typename C::MmWide>(a, s);
-  return launch_stage_g<E, typename C::LogitsTail, typename C::Mm, typename C::MmWide>(a, s);
+  if (whole) return launch_stage_g<E, ENT, typename C::Logits, typename C::Mm, typename C::MmWide>(a, s);
+  return launch_stage_g<E, ENT, typename C::LogitsTail, typename C::Mm, typename C::MmWide>(a, s);
 }
 
 }  // namespace vpce

@@ -18,6 +18,11 @@ struct NormArgs {
   int64_t T;
   int32_t d;
   float eps;
+  // with a residual (vp_add_norm_forward): X + R is what is normalised
+  const void* R;   // [T, d], null without
+  void* S;         // [T, d]: the sum
+  uint8_t* Y8;     // [T, d] or null; Y may then be null
+  uint8_t* scale;  // [T][(d + 127) / 128]
 };
 
 struct NormGradArgs {
@@ -33,11 +38,12 @@ struct NormGradArgs {
   int64_t T;
   int32_t d;
   int32_t accumulate;
+  const float* dS;  // [T, d] added to dX, may be dX; null for none
 };
 
 // Rows of partial sums of dgamma (and of dbeta) that a backward writes.
 int norm_parts(int64_t T, int d);
-bool run_norm_forward(int dtype, bool rms, const NormArgs& a, hipStream_t s);
+bool run_norm_forward(int dtype, bool rms, const NormArgs& a, hipStream_t s);  // (a.R: with a residual)
 bool run_norm_backward(int dtype, bool rms, const NormGradArgs& a, hipStream_t s);
 
 // T packed tokens in S sequences (start [S + 1]); see vpce.h.

@@ -32,6 +32,21 @@ size_t norm_ws_bytes(const vp_norm* n) {
   return 256 + 2 * (size_t)vpce::norm_parts(n->T, (int)n->d) * (size_t)n->d * 4;
 }
 
+vpce::NormArgs norm_args(const vp_norm* norm, const void* X, const void* gamma, const void* beta, void* Y,
+                         float* mean, float* rstd) {
+  vpce::NormArgs a{};
+  a.X = X;
+  a.gamma = gamma;
+  a.beta = beta;
+  a.Y = Y;
+  a.mean = norm->flags & VP_NORM_RMS ? nullptr : mean;
+  a.rstd = rstd;
+  a.T = norm->T;
+  a.d = (int32_t)norm->d;
+  a.eps = (float)norm->eps;
+  return a;
+}
+
 vp_status validate(const vp_sequences* q) {
   if (!q) return VP_ERR_NULL;
   if (q->T < 0 || q->T > kMaxT || q->S < 0 || q->S > kMaxS) return VP_ERR_SHAPE;
@@ -133,29 +148,45 @@ vp_status vp_norm_forward(const vp_norm* norm, const void* X, const void* gamma,
   if (!X || !gamma || !Y || !rstd || (!rms && !mean)) return VP_ERR_NULL;
   if (off(X, 16) || off(gamma, 16) || off(beta, 16) || off(Y, 16)) return VP_ERR_ALIGN;
   if (off(rstd, 4) || (!rms && off(mean, 4))) return VP_ERR_ALIGN;
-  vpce::NormArgs a;
-  a.X = X;
-  a.gamma = gamma;
-  a.beta = beta;
-  a.Y = Y;
-  a.mean = rms ? nullptr : mean;
-  a.rstd = rstd;
-  a.T = norm->T;
-  a.d = (int32_t)norm->d;
-  a.eps = (float)norm->eps;
+  vpce::NormArgs a = norm_args(norm, X, gamma, beta, Y, mean, rstd);
   return vpce::run_norm_forward(norm->dtype, rms, a, (hipStream_t)stream) ? VP_OK : VP_ERR_HIP;
 }
 
-vp_status vp_norm_backward(const vp_norm* norm, const void* X, const void* gamma, const float* mean,
-                           const float* rstd, const float* dY, float* dX, float* dgamma,
-                           float* dbeta, void* ws, size_t ws_bytes, void* stream) {
+vp_status vp_add_norm_forward(const vp_norm* norm, const void* X, const void* R, const void* gamma,
+                              const void* beta, void* S, void* Y, void* Y8, uint8_t* scale,
+                              float* mean, float* rstd, void* stream) {
+  const vp_status st = validate(norm);
+  if (st != VP_OK) return st;
+  const bool rms = (norm->flags & VP_NORM_RMS) != 0;
+  if (norm->T == 0) return VP_OK;
+  if (!X || !R || !gamma || !S || !rstd || (!rms && !mean)) return VP_ERR_NULL;
+  if ((!Y && !Y8) || !Y8 != !scale) return VP_ERR_NULL;
+  if (off(X, 16) || off(R, 16) || off(gamma, 16) || off(beta, 16) || off(S, 16) || off(Y, 16) || off(Y8, 16))
+    return VP_ERR_ALIGN;
+  if (off(rstd, 4) || (!rms && off(mean, 4))) return VP_ERR_ALIGN;
+  vpce::NormArgs a = norm_args(norm, X, gamma, beta, Y, mean, rstd);
+  a.R = R;
+  a.S = S;
+  a.Y8 = (uint8_t*)Y8;
+  a.scale = scale;
+  return vpce::run_norm_forward(norm->dtype, rms, a, (hipStream_t)stream) ? VP_OK : VP_ERR_HIP;
+}
+
+}  // extern "C"
+
+namespace {
+
+vp_status norm_backward(const vp_norm* norm, const void* X, const void* gamma, const float* mean,
+                        const float* rstd, const float* dY, const float* dS, float* dX, float* dgamma,
+                        float* dbeta, void* ws, size_t ws_bytes, void* stream) {
   vp_status st = validate(norm);
   if (st != VP_OK) return st;
   const bool rms = (norm->flags & VP_NORM_RMS) != 0;
   if ((st = check_ws(ws, ws_bytes, norm_ws_bytes(norm))) != VP_OK) return st;
   if (!gamma || !dgamma) return VP_ERR_NULL;
   if (norm->T > 0 && (!X || !rstd || !dY || !dX || (!rms && !mean))) return VP_ERR_NULL;
-  if (off(X, 16) || off(gamma, 16) || off(dY, 16) || off(dX, 16) || off(dgamma, 16) || off(dbeta, 16))
+  if (off(X, 16) || off(gamma, 16) || off(dY, 16) || off(dS, 16) || off(dX, 16) || off(dgamma, 16) ||
+      off(dbeta, 16))
     return VP_ERR_ALIGN;
   if (off(rstd, 4) || (!rms && off(mean, 4))) return VP_ERR_ALIGN;
   vpce::NormGradArgs a;
@@ -171,7 +202,25 @@ vp_status vp_norm_backward(const vp_norm* norm, const void* X, const void* gamma
   a.T = norm->T;
   a.d = (int32_t)norm->d;
   a.accumulate = (norm->flags & VP_ACCUMULATE_DW) != 0;
+  a.dS = dS;
   return vpce::run_norm_backward(norm->dtype, rms, a, (hipStream_t)stream) ? VP_OK : VP_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+vp_status vp_norm_backward(const vp_norm* norm, const void* X, const void* gamma, const float* mean,
+                           const float* rstd, const float* dY, float* dX, float* dgamma,
+                           float* dbeta, void* ws, size_t ws_bytes, void* stream) {
+  return norm_backward(norm, X, gamma, mean, rstd, dY, nullptr, dX, dgamma, dbeta, ws, ws_bytes, stream);
+}
+
+vp_status vp_add_norm_backward(const vp_norm* norm, const void* S, const void* gamma,
+                               const float* mean, const float* rstd, const float* dY,
+                               const float* dS, float* dX, float* dgamma, float* dbeta, void* ws,
+                               size_t ws_bytes, void* stream) {
+  return norm_backward(norm, S, gamma, mean, rstd, dY, dS, dX, dgamma, dbeta, ws, ws_bytes, stream);
 }
 
 vp_status vp_seq_workspace_size(const vp_sequences* seq, size_t* bytes) {

@@ -44,6 +44,59 @@ struct CombArgs {
   unsigned long long* bad_counter;
 };
 
+// Tiles the forward can run on: kind 0 is the 256 x 256 tile of every large problem,
+// the others are the streamed tiles for few tokens.
+constexpr int kFwdKinds = 3;
+struct FwdTile {
+  int bm, bn;             // vocabulary rows by tokens
+  int per_cu;             // workgroups a CU holds
+  double shared, stream;  // time per slice: W shared by several token blocks, or by none
+};
+FwdTile fwd_tile(int dtype, int kind);
+
+// A scoring forward (vp_score_forward): the forward with the sum that the entropy needs and,
+// for alternatives, the maxima of every four consecutive logits (fine) and of the logits that
+// a lane of a tile holds (coarse), by tile and token.  A tile of bm vocabulary rows has bm / 4
+// fine maxima and cpt coarse ones; coarse maximum c covers the fine ones (c / 2) (fpc) + 2 k +
+// c % 2 of them for k < fpc = bm / 4 / cpt, counted from (c / 2) (2 fpc).
+struct ScoreArgs {
+  FwdArgs f;
+  float* u_part;  // [n_splits][T]: sum of 2^x x, x the exponent (below 0) in s_part's sum
+  float* fine;    // [n_tiles][T][bm / 4], NaN where no row is live; null without alternatives
+  float* coarse;  // [n_tiles][T][cpt]
+  // 8-bit operands: scales of H [T][nb] and of each shard in the table's order [rows / 128][nb]
+  const uint8_t* h_scale;
+  const uint8_t* w_scale[VP_MAX_SHARDS];
+  int32_t nb;
+};
+
+constexpr int kF8MaxBlocks = 112;  // 128-column blocks that a token's scales may be of
+constexpr int kF8MaxD = 128 * kF8MaxBlocks;
+
+struct ScoreCombArgs {
+  CombArgs c;
+  const float* u_part;
+  float* entropy;  // may be null
+};
+
+struct TopArgs {
+  ScoreArgs s;
+  const float* lse;
+  int32_t bm, cpt, top;
+  int64_t* ids;  // [T][top]
+  float* loss;   // [T][top]
+};
+
+// Quantisation to 8 bits (vp_f8_quantize).
+struct QuantArgs {
+  const void* X;   // [rows, cols]
+  uint8_t* X8;     // [rows, cols]
+  uint8_t* scale;  // [rows or 128-row blocks][nb]
+  int64_t rows;
+  int32_t cols, nb;
+};
+bool run_quantize(int dtype, const QuantArgs& a, int rows_per_scale, hipStream_t s);
+
 // Per-token fold state of Algorithm 2 as the ABI exposes it: float32 [3][T],
 // planes m (running maximum logit, natural units), s (sum of e^(y - m) over the
 // ids folded so far) and y (the target logit once its shard has been folded).
@@ -154,6 +207,8 @@ struct StageArgs {
   const void *Wt, *Ht;  // class 3: k-blocked transposed copies of its W rows and of H
   float* part;         // [jobs][T][d], or dH itself for one job
   int64_t part_stride;
+  // entropy of every token and the upstream gradient of it; both null for a loss alone
+  const float *entropy, *grad_entropy;
 };
 // Tile classes: 0 (bfloat16): 256 x 256 tiles; 1: 128 x 64 ones; 2: 128 x 128 ones, all of
 // them with W and H read transposed; 3: 256 x 256 tiles on transposed copies.
@@ -165,18 +220,9 @@ struct BwdTile {
 BwdTile bwd_tile(int dtype, int cls);
 int bwd_col_blocks(int cls, int d);  // column blocks of the contractions
 bool run_stage(int dtype, int cls, const StageArgs& a, hipStream_t s);
+bool run_stage_entropy(int dtype, int cls, const StageArgs& a, hipStream_t s);  // (a.grad_entropy)
 // out[i] = sum over k < n of part[k * len + i], in the order of k; len % 4 == 0
 bool run_sum_parts(const float* part, int n, int64_t len, float* out, hipStream_t s);
-
-// Tiles the forward can run on: kind 0 is the 256 x 256 tile of every large problem,
-// the others are the streamed tiles for few tokens.
-constexpr int kFwdKinds = 3;
-struct FwdTile {
-  int bm, bn;             // vocabulary rows by tokens
-  int per_cu;             // workgroups a CU holds
-  double shared, stream;  // time per slice: W shared by several token blocks, or by none
-};
-FwdTile fwd_tile(int dtype, int kind);
 
 // Bytes of the library-owned device workspace of vp_ce_forward_noalloc.
 constexpr size_t kScratchBytes = 16u << 20;
@@ -187,6 +233,11 @@ bool run_ws_init(unsigned long long* counter, hipStream_t s);
 bool run_fill_zero(float* p, int64_t n, hipStream_t s);
 bool run_fwd(int dtype, const FwdArgs& a, hipStream_t s);
 bool run_comb(const CombArgs& a, hipStream_t s);
+int score_coarse(int kind);  // coarse maxima of a tile
+FwdTile score_tile_f8(int kind);  // kinds 0 and 2
+bool run_score(int dtype, const ScoreArgs& a, hipStream_t s);
+bool run_score_comb(int dtype, const ScoreCombArgs& a, const ScoreArgs& sa, hipStream_t s);
+bool run_top(int dtype, const TopArgs& a, hipStream_t s);
 bool run_state_init(float* state, int64_t T, hipStream_t s);
 bool run_fold_merge(const FoldArgs& a, hipStream_t s);
 bool run_fold_finalize(const FinArgs& a, hipStream_t s);

@@ -511,6 +511,7 @@ static FwdTile fwd_tile_of(int kind) {
   return b16 ? FwdTile{G0::BM, G0::BN, G0::OCC, 1.4, 1.8} : FwdTile{G0::BM, G0::BN, G0::OCC, 7.45, 7.45};
 }
 FwdTile fwd_tile(int dtype, int kind) {
+  if (dtype == VP_E4M3) return score_tile_f8(kind);
   return dtype == 1 ? fwd_tile_of<Bf16>(kind) : fwd_tile_of<F32>(kind);
 }
 
@@ -532,7 +533,8 @@ BwdTile bwd_tile(int dtype, int cls) {
   return BwdTile{B::Tr256::BM, B::Tr256::BN, 1.40};
 }
 bool run_stage(int dtype, int cls, const StageArgs& a, hipStream_t s) {
-  return dtype == 1 ? launch_stage<Bf16>(cls, a, s) : launch_stage<F32>(cls, a, s);
+  if (a.grad_entropy) return run_stage_entropy(dtype, cls, a, s);
+  return dtype == 1 ? launch_stage<Bf16, false>(cls, a, s) : launch_stage<F32, false>(cls, a, s);
 }
 bool run_sum_parts(const float* part, int n, int64_t len, float* out, hipStream_t s) {
   const int64_t vecs = len / 4, blocks = std::min<int64_t>((vecs + 255) / 256, 2048);

@@ -20,6 +20,7 @@
 
 #include <algorithm>
 
+#include "vpce_f8.h"
 #include "vpce_head.h"
 #include "vpce_lanes.h"
 
@@ -105,7 +106,48 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*red)[N][W], int& 
   }
 }
 
-template <class E, bool RMS, int LANES, int EL>
+// The row y in 8 bits: the lanes that share 128 columns find their largest magnitude, and with it
+// the scale.  A block is 128 / VEC consecutive vectors, i.e. as many lanes, or the LANES of a narrow
+// row with all their vectors.
+template <class E, int LANES, int EL>
+__device__ __forceinline__ void store_f8(const NormArgs& a, int64_t t, int lane, const float (&y)[EL / E::VEC][E::VEC]) {
+  constexpr int VEC = E::VEC, NV = EL / VEC;
+  constexpr int GRP = LANES < 128 / VEC ? LANES : 128 / VEC;
+  constexpr int KS = GRP < 128 / VEC ? NV : 1;  // vectors of a lane in a block
+  static_assert(GRP == 128 / VEC || LANES * EL <= 128, "a block is whole in its lanes");
+  const int nvec = a.d / VEC, nb = (a.d + 127) / 128;
+#pragma unroll
+  for (int k0 = 0; k0 < NV; k0 += KS) {
+    float m = 0.f;
+#pragma unroll
+    for (int k = k0; k < k0 + KS; ++k)
+      if (lane + k * LANES < nvec)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) m = fmaxf(m, finite_magnitude(y[k][j]));
+    const int b = f8_scale(lanes_max<GRP>(m));
+    const float inverse = f8_inverse(b);
+#pragma unroll
+    for (int k = k0; k < k0 + KS; ++k) {
+      const int i = lane + k * LANES;
+      if (i >= nvec) continue;
+      uint32_t* out = (uint32_t*)(a.Y8 + t * a.d) + i * (VEC / 4);
+      uint32_t w[VEC / 4];
+#pragma unroll
+      for (int q = 0; q < VEC / 4; ++q)
+        w[q] = f8_pack4(y[k][4 * q] * inverse, y[k][4 * q + 1] * inverse, y[k][4 * q + 2] * inverse,
+                        y[k][4 * q + 3] * inverse);
+      if constexpr (VEC == 8)
+        *(uint2*)out = make_uint2(w[0], w[1]);
+      else
+        *out = w[0];
+    }
+    const int i = lane + k0 * LANES;
+    if (lane % GRP == 0 && i < nvec) a.scale[t * nb + i / (128 / VEC)] = (uint8_t)b;
+  }
+}
+
+// ADD: X + R, rounded, is stored and normalised, and y may leave in 8 bits.
+template <class E, bool RMS, int LANES, int EL, bool ADD>
 __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(NormArgs a) {
   using R = Row<E, LANES, EL>;
   constexpr int VEC = R::VEC, NV = R::NV;
@@ -122,6 +164,15 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(N
   for (int k = 0; k < NV; ++k) {
     const int i = lane + k * R::LANES;
     E::unpack(i < nvec ? x[i] : make_uint4(0, 0, 0, 0), f[k]);
+    if constexpr (ADD) {
+      float r[VEC];
+      E::unpack(i < nvec ? ((const uint4*)a.R + t * nvec)[i] : make_uint4(0, 0, 0, 0), r);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) f[k][j] += r[j];
+      const uint4 sum = E::pack(f[k]);
+      if (i < nvec) ((uint4*)a.S + t * nvec)[i] = sum;
+      E::unpack(sum, f[k]);
+    }
   }
   const float inv_d = 1.f / (float)a.d;
   float mean = 0.f, left = 0.f;
@@ -169,10 +220,13 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(N
       for (int j = 0; j < VEC; ++j) {
         const float xh = RMS ? f[k][j] * rstd : __builtin_fmaf(f[k][j], rstd, shift);
         ga[j] = a.beta ? __builtin_fmaf(xh, ga[j], be[j]) : xh * ga[j];
+        if constexpr (ADD) f[k][j] = ga[j];
       }
-      y[i] = E::pack(ga);
+      if (!ADD || a.Y) y[i] = E::pack(ga);
     }
   }
+  if constexpr (ADD)
+    if (a.Y8) store_f8<E, LANES, EL>(a, t, lane, f);
   if (lane == 0) {
     a.rstd[t] = rstd;
     if (!RMS) a.mean[t] = mean + left;
@@ -183,7 +237,7 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_forward_kernel(N
 // is a single wavefront) with the sums of dgamma and dbeta over them in registers, and
 // leaves these as one row of partial sums each (or the result, where it is alone).  The
 // order of every sum depends on the sizes alone: the same call gives the same bits.
-template <class E, bool RMS, int LANES, int EL>
+template <class E, bool RMS, int LANES, int EL, bool ADD>
 __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(NormGradArgs a) {
   using R = Row<E, LANES, EL>;
   constexpr int VEC = R::VEC, NV = R::NV;
@@ -205,7 +259,7 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(
     for (int j = 0; j < VEC; ++j) dg[k][j] = db[k][j] = 0.f;
   }
   uint4 xn[NV];
-  float4 dyn[NV][VEC / 4];
+  float4 dyn[NV][VEC / 4], dsn[ADD ? NV : 1][VEC / 4];
   float mean_n = 0.f, rstd_n = 0.f;
   auto load = [&](int64_t t) {
     if (t >= a.T) return;
@@ -217,7 +271,10 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(
       if (i < nvec) {
         xn[k] = x[i];
 #pragma unroll
-        for (int q = 0; q < VEC / 4; ++q) dyn[k][q] = dy[i * (VEC / 4) + q];
+        for (int q = 0; q < VEC / 4; ++q) {
+          dyn[k][q] = dy[i * (VEC / 4) + q];
+          if constexpr (ADD) dsn[k][q] = ((const float4*)a.dS + t * (a.d / 4))[i * (VEC / 4) + q];
+        }
       }
     }
     if (!RMS) mean_n = a.mean[t];
@@ -229,12 +286,14 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(
     if (!AHEAD) load(t);
     uint4 xr[NV];
     float dy[NV][VEC];
+    float4 ds[ADD ? NV : 1][VEC / 4];
     const float mean = mean_n, rstd = rstd_n;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       xr[k] = xn[k];
 #pragma unroll
       for (int q = 0; q < VEC / 4; ++q) {
+        if constexpr (ADD) ds[k][q] = dsn[k][q];
         dy[k][4 * q] = dyn[k][q].x;
         dy[k][4 * q + 1] = dyn[k][q].y;
         dy[k][4 * q + 2] = dyn[k][q].z;
@@ -272,6 +331,7 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(
         for (int j = 0; j < VEC; ++j) {
           const float xh = (x[j] - mean) * rstd;
           g[j] = rstd * (g[j] * dy[k][j] - c1 - xh * c2);
+          if constexpr (ADD) g[j] += ((const float*)&ds[k][j / 4])[j % 4];
         }
 #pragma unroll
         for (int q = 0; q < VEC / 4; ++q)
@@ -397,7 +457,7 @@ bool backward_layout(int d, F&& f) {
   return f.template run<1024, 16>();
 }
 
-template <class E, bool RMS>
+template <class E, bool RMS, bool ADD>
 struct Forward {
   const NormArgs& a;
   hipStream_t s;
@@ -410,19 +470,26 @@ struct Forward {
     for (int64_t t = 0; t < a.T; t += kRows) {
       NormArgs b = a;
       b.T = std::min(kRows, a.T - t);
-      b.X = (const typename E::storage*)a.X + t * a.d;
-      b.Y = (typename E::storage*)a.Y + t * a.d;
+      using S = typename E::storage;
+      b.X = (const S*)a.X + t * a.d;
+      b.Y = a.Y ? (S*)a.Y + t * a.d : nullptr;
       b.mean = RMS ? nullptr : a.mean + t;
       b.rstd = a.rstd + t;
-      hipLaunchKernelGGL((norm_forward_kernel<E, RMS, LANES, EL>), dim3((unsigned)((b.T + R::ROWS - 1) / R::ROWS)),
-                         dim3(R::NT), 0, s, b);
+      if constexpr (ADD) {
+        b.R = (const S*)a.R + t * a.d;
+        b.S = (S*)a.S + t * a.d;
+        b.Y8 = a.Y8 ? a.Y8 + t * a.d : nullptr;
+        b.scale = a.Y8 ? a.scale + t * ((a.d + 127) / 128) : nullptr;
+      }
+      hipLaunchKernelGGL((norm_forward_kernel<E, RMS, LANES, EL, ADD>),
+                         dim3((unsigned)((b.T + R::ROWS - 1) / R::ROWS)), dim3(R::NT), 0, s, b);
       if (!launched_ok()) return false;
     }
     return true;
   }
 };
 
-template <class E, bool RMS>
+template <class E, bool RMS, bool ADD>
 struct Backward {
   const NormGradArgs& a;
   hipStream_t s;
@@ -430,7 +497,7 @@ struct Backward {
   bool run() {
     using R = Row<E, LANES, EL>;
     const int n = norm_parts(a.T, a.d);
-    hipLaunchKernelGGL((norm_backward_kernel<E, RMS, LANES, EL>), dim3((unsigned)n), dim3(R::NT), 0, s, a);
+    hipLaunchKernelGGL((norm_backward_kernel<E, RMS, LANES, EL, ADD>), dim3((unsigned)n), dim3(R::NT), 0, s, a);
     if (!launched_ok()) return false;
     if (n == 1) return true;
     hipLaunchKernelGGL(norm_weight_grad_kernel, dim3((unsigned)((a.d + 63) / 64), a.dbeta ? 2u : 1u), dim3(1024), 0, s,
@@ -467,19 +534,23 @@ int norm_parts(int64_t T, int d) {
   return (int)std::max<int64_t>(std::min<int64_t>(rounds, p.n), (rounds + 1023) / 1024);
 }
 
+template <bool RMS, bool ADD>
+static bool forward_of(int dtype, const NormArgs& a, hipStream_t s) {
+  return dtype == VP_BF16 ? forward_layout<Half>(a.d, Forward<Half, RMS, ADD>{a, s})
+                          : forward_layout<Single>(a.d, Forward<Single, RMS, ADD>{a, s});
+}
 bool run_norm_forward(int dtype, bool rms, const NormArgs& a, hipStream_t s) {
-  if (dtype == VP_BF16)
-    return rms ? forward_layout<Half>(a.d, Forward<Half, true>{a, s})
-               : forward_layout<Half>(a.d, Forward<Half, false>{a, s});
-  return rms ? forward_layout<Single>(a.d, Forward<Single, true>{a, s})
-             : forward_layout<Single>(a.d, Forward<Single, false>{a, s});
+  if (a.R) return rms ? forward_of<true, true>(dtype, a, s) : forward_of<false, true>(dtype, a, s);
+  return rms ? forward_of<true, false>(dtype, a, s) : forward_of<false, false>(dtype, a, s);
+}
+template <bool RMS, bool ADD>
+static bool backward_of(int dtype, const NormGradArgs& a, hipStream_t s) {
+  return dtype == VP_BF16 ? backward_layout(a.d, Backward<Half, RMS, ADD>{a, s})
+                          : backward_layout(a.d, Backward<Single, RMS, ADD>{a, s});
 }
 bool run_norm_backward(int dtype, bool rms, const NormGradArgs& a, hipStream_t s) {
-  if (dtype == VP_BF16)
-    return rms ? backward_layout(a.d, Backward<Half, true>{a, s})
-               : backward_layout(a.d, Backward<Half, false>{a, s});
-  return rms ? backward_layout(a.d, Backward<Single, true>{a, s})
-             : backward_layout(a.d, Backward<Single, false>{a, s});
+  if (a.dS) return rms ? backward_of<true, true>(dtype, a, s) : backward_of<false, true>(dtype, a, s);
+  return rms ? backward_of<true, false>(dtype, a, s) : backward_of<false, false>(dtype, a, s);
 }
 
 }  // namespace vpce

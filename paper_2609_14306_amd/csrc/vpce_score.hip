@@ -1,0 +1,884 @@
+// Scoring of tokens, for gfx950 (MI355X): the forward of the vocabulary projection (see
+// vpce_kernels.hip) with the entropy of every token and its most likely ids, in bfloat16, float32
+// and 8-bit floating point.
+//
+// Entropy.  With the running maximum m and s = sum 2^x, x = y log2e - m, the fold keeps u =
+// sum 2^x x as well; where m grows by c, s' = s 2^-c and u' = 2^-c (u - c s).  Then
+//   lse = ln2 (m + log2 s),   entropy = lse - sum p y = ln2 (log2 s - u / s),
+// a sum of two terms that are not negative: nothing cancels.
+//
+// Alternatives.  No logits are kept; the fold leaves the maximum of every four consecutive ids
+// (fine) and of the logits that a lane holds of a tile (coarse).  The K + 4 largest fine maxima,
+// ties by the lower ids, hold the K largest logits but for what float32 sums round: the logits of
+// those ids are taken again in float64, where the products of the operands are exact, and ranked by
+// that.  An answer differs from the float64 one only where five groups of ids lie within the
+// rounding of a float32 sum at its border.
+//
+// 8-bit operands (e4m3) have a power of two as scale for every 128 columns of a token and every 128
+// x 128 block of a shard.  A slice of 128 bytes is one such block: the matrix instruction of
+// 64 columns takes the scales as its own operands, for nothing.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "vpce_internal.h"
+#include "vpce_tiles.h"
+
+namespace vpce {
+
+// 8-bit elements: a 128-byte slice row is 128 columns, one scale.
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+struct F8 {
+  using storage = uint8_t;
+  using frag16 = i32x4_t;
+  static constexpr int VEC = 16, KB = 128;
+  // 64 columns: a lane holds 32 of them, two 16-byte chunks, the same ones in both operands.
+  __device__ static i32x8_t join(frag16 x, frag16 y) {
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  __device__ static f32x16_t mma(i32x8_t a, i32x8_t b, f32x16_t c, int sa, int sb) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
+  }
+};
+template <class E>
+constexpr bool kIsF8 = sizeof(typename E::storage) == 1;
+
+// Scales in LDS: of the BN tokens of a workgroup, [nb][BN], and of as many of its vocabulary
+// tiles as have room, [tile][128-row block][nb].
+template <class G>
+struct Scales {
+  static constexpr int BLOCKS = G::BM / 128;
+  static constexpr int H_BYTES = G::BN * kF8MaxBlocks;
+  static constexpr int W_BYTES = (160 * 1024 - G::LDS_ELEMS - H_BYTES) / 16 * 16;
+  static_assert(W_BYTES >= BLOCKS * kF8MaxBlocks, "one tile's scales");
+  uint8_t *h, *w;
+  int nb, first, count;  // tiles whose scales are there
+
+  __device__ __forceinline__ void load_tokens(const ScoreArgs& a, int n0) {
+    nb = a.nb;
+    first = count = 0;
+    for (int i = threadIdx.x; i < G::BN * nb; i += G::NT) {
+      const int64_t n = n0 + i / nb;
+      h[(i % nb) * G::BN + i / nb] = a.h_scale[(n < a.f.T ? n : a.f.T - 1) * nb + i % nb];
+    }
+  }
+  // Scales of the tiles from ti on, before end; all threads, and no other is between barriers.
+  __device__ __forceinline__ void load_tiles(const ScoreArgs& a, int ti, int end) {
+    first = ti;
+    count = min(end - ti, W_BYTES / (BLOCKS * nb));
+    __syncthreads();
+    for (int i = threadIdx.x; i < count * BLOCKS * nb; i += G::NT) {
+      const int b = i / nb, tile = ti + b / BLOCKS;
+      int pos = 0;
+      while (tile >= a.f.st.tile0[pos + 1]) ++pos;
+      const int row = (tile - a.f.st.tile0[pos]) * BLOCKS + b % BLOCKS;
+      const int rows = (a.f.st.rows[pos] + 127) / 128;
+      w[i] = a.w_scale[pos][(int64_t)min(row, rows - 1) * nb + i % nb];
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ bool has(int ti) const { return ti >= first && ti < first + count; }
+  __device__ __forceinline__ int of_rows(int ti, int wm, int kt) const {
+    return w[((ti - first) * BLOCKS + wm / 128) * nb + kt];
+  }
+  __device__ __forceinline__ int of_token(int column, int kt) const { return h[kt * G::BN + column]; }
+};
+
+struct NoScales {};
+template <class E, class G>
+using ScalesFor = std::conditional_t<kIsF8<E>, Scales<G>, NoScales>;
+
+// The 256 x 256 tile of GemmDma for 8-bit operands: its slices, swizzle and loads, two sub-steps
+// of 64 columns a slice.  All loads of slice kt + 2 go out during the second sub-step of slice kt,
+// one behind each of its first MFMAs, and have the first sub-step of slice kt + 1 to land.
+template <bool KTAIL_>
+struct GemmF8 : GemmDma<256, 256, 2, 4, F8, KTAIL_> {
+  using Base = GemmDma<256, 256, 2, 4, F8, KTAIL_>;
+  using typename Base::F16;
+  using typename Base::Loads;
+  using typename Base::S;
+  using Base::BK, Base::KTAIL, Base::MB, Base::NB, Base::NLOADS, Base::NM, Base::STAGES;
+  using Base::issue_one, Base::plan, Base::read_one, Base::slot_bytes, Base::wait_slices;
+
+  __device__ __forceinline__ static void run(f32x16_t (&acc)[MB][NB], const S* __restrict__ A, int64_t lda,
+                                             int M, const S* __restrict__ B, int64_t ldb, int n0, int N, int K,
+                                             char* smem, const Scales<GemmF8>& sc, int ti) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = Base::wave_m(wave), wn = Base::wave_n(wave);
+    const int nk = (K + BK - 1) / BK;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    Loads L;
+    plan(L, A, lda, 0, M, B, ldb, n0, N, wave, lane);
+    L.kblkA = L.kblkB = BK;
+    if constexpr (KTAIL) {
+      L.tail_kt = K % BK ? nk - 1 : -1;
+      L.tail_chunks = K % BK / F8::VEC;
+    }
+    const int pro = min(STAGES, nk);
+    for (int kt = 0; kt < pro; ++kt)
+#pragma unroll
+      for (int q = 0; q < NLOADS; ++q) issue_one(L, kt, q, lds0, wave);
+    wait_slices(pro - 1);
+    __builtin_amdgcn_s_barrier();
+    const char* ring = smem;
+    // fragment idx (A's row blocks, then B's) of the sub-step that begins with chunks 2 kk
+    auto read = [&](const char* slot, int kk, int idx) {
+      return F8::join(read_one(slot, wm, wn, kk, lane, idx), read_one(slot, wm, wn, kk + 1, lane, idx));
+    };
+    i32x8_t a[MB], b[2][NB];
+    int sa, sb[NB], sa_next, sb_next[NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) a[i] = read(ring, 0, i);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) b[0][j] = read(ring, 0, MB + j);
+    sa_next = sc.of_rows(ti, wm, 0);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) sb_next[j] = sc.of_token(wn + 32 * j + (lane & 31), 0);
+    for (int kt = 0; kt < nk; ++kt) {
+      sa = sa_next;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) sb[j] = sb_next[j];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const char* src;
+        int skk;
+        if (kk == 0) {
+          src = ring + slot_bytes(kt);
+          skk = 2;
+          const int next = min(kt + 1, nk - 1);
+          sa_next = sc.of_rows(ti, wm, next);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) sb_next[j] = sc.of_token(wn + 32 * j + (lane & 31), next);
+        } else {
+          // as in GemmDma::run: slice kt + 1 has landed, and on the last slice a spare barrier
+          wait_vmcnt<0>();
+          wait_lgkmcnt0();
+          __builtin_amdgcn_s_barrier();
+          src = ring + slot_bytes(kt + 1);
+          skk = 0;
+        }
+        const bool loads = kk == 1 && kt + STAGES < nk;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int idx = 0; idx < NM; ++idx) {
+          const int i = idx / NB, jj = idx % NB, j = (i & 1) ? NB - 1 - jj : jj;
+          acc[i][j] = F8::mma(a[i], b[kk][j], acc[i][j], sa, sb[j]);
+          // (an empty statement that keeps the product in front of the branches around the loads:
+          // the compiler would move all sixteen of a slice behind them)
+          asm volatile("" : "+v"(acc[i][j]));
+          __builtin_amdgcn_sched_barrier(0);
+          if (idx < NB) b[kk ^ 1][idx] = read(src, skk, MB + idx);
+          if (jj == NB - 1) a[i] = read(src, skk, i);
+          if (loads && idx < NLOADS) issue_one(L, kt + STAGES, idx, lds0, wave);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    wait_vmcnt<0>();
+    wait_lgkmcnt0();
+    __builtin_amdgcn_s_barrier();
+  }
+  static_assert(NLOADS <= NM, "one load behind each MFMA");
+};
+
+// The streamed tile of Ring for 8-bit operands.
+struct RingF8 : Ring<128, 64, 4, 2, 6, F8> {
+  __device__ __forceinline__ static void multiply(f32x16_t (&acc)[MB][NB], const char* slot, int wm, int wn,
+                                                  int lane, int sa, const int (&sb)[NB]) {
+#pragma unroll
+    for (int kk = 0; kk < 4; kk += 2) {
+      auto read = [&](int first, int r) {
+        const char* row = slot + (first + r) * 128;
+        const int chunk = 2 * kk + (lane >> 5);
+        return F8::join(*(const F16*)(row + ((chunk ^ key(r)) << 4)), *(const F16*)(row + (((chunk + 2) ^ key(r)) << 4)));
+      };
+      i32x8_t fa[MB], fb[NB];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) fa[i] = read(0, wm + 32 * i + (lane & 31));
+#pragma unroll
+      for (int j = 0; j < NB; ++j) fb[j] = read(BM, wn + 32 * j + (lane & 31));
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = F8::mma(fa[i], fb[j], acc[i][j], sa, sb[j]);
+    }
+  }
+};
+
+template <> struct Cfg<F8> {
+  using Logits = GemmF8<false>;
+  using LogitsTail = GemmF8<true>;
+  using Stream64 = RingF8;
+};
+
+// ---------------------------------------------------------------------------
+// A lane's state of a token: maximum, sum and sum of 2^x x (base-2 domain).
+struct Fold {
+  float m, s, u;
+};
+constexpr float kLeast = -1e4f;  // 2^kLeast is 0: the x of a logit of minus infinity
+__device__ __forceinline__ void rescale(Fold& f, float m) {
+  const float c = f.m - m, e = __builtin_amdgcn_exp2f(c);
+  f.s *= e;
+  f.u = __builtin_fmaf(f.u, e, f.s > 0.f ? c * f.s : 0.f);  // (an empty state's c may be infinite)
+  f.m = m;
+}
+__device__ __forceinline__ void merge_fold(Fold& f, Fold o) {
+  const float m = fmaxf(f.m, o.m), ref = m == -INFINITY ? 0.f : m;
+  rescale(f, ref);
+  rescale(o, ref);
+  f.m = m;
+  f.s += o.s;
+  f.u += o.u;
+}
+
+// Folds column block j of a logits tile (fold_tile of vpce_tiles.h with the third sum) and, with
+// TOP, leaves its maxima: fine, the bm / 4 ones of this tile and the lane's token, and coarse
+// (both null for a token that does not exist).  Rows from `lim` on are minus infinity.
+template <int MB, int NB, bool TOP>
+__device__ __forceinline__ void fold_score(const f32x16_t (&acc)[MB][NB], int j, bool full, int lim, Fold& f,
+                                           int lane, float* fine, float* coarse) {
+  float g[MB][4], top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x16_t& v = acc[i][j];
+      g[i][q] = fmaxf(fmaxf(v[4 * q], v[4 * q + 1]), fmaxf(v[4 * q + 2], v[4 * q + 3]));
+      top = fmaxf(top, g[i][q]);
+    }
+  }
+  if constexpr (TOP) {
+    if (coarse) *coarse = top;
+    if (!full)
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) g[i][q] = 32 * i + 8 * q < lim ? g[i][q] : __builtin_nanf("");
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      // The lanes l and l + 32 hold the even and the odd ones of the block's eight maxima; after
+      // two swaps of half wavefronts they hold the first and the last four.
+      typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+      const u32x2_t x = __builtin_bit_cast(
+          u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(g[i][0]), __float_as_uint(g[i][2]), false, false));
+      const u32x2_t y = __builtin_bit_cast(
+          u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(g[i][1]), __float_as_uint(g[i][3]), false, false));
+      if (fine)
+        *(float4*)(fine + 8 * i + 4 * (lane >> 5)) =
+            make_float4(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(y[0]), __uint_as_float(y[1]));
+    }
+  }
+  const float tmax = top * kLog2e;
+  rescale(f, fmaxf(f.m, tmax));
+  float s = 0.f, u = 0.f;
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    __builtin_amdgcn_sched_barrier(0);  // (16 exponents at a time: more of them are spilled)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float x = __builtin_fmaf(acc[i][j][r], kLog2e, -f.m), e = __builtin_amdgcn_exp2f(x);
+      s += e;
+      u = __builtin_fmaf(e, fmaxf(x, kLeast), u);
+    }
+  }
+  f.s += s;
+  f.u += u;
+}
+
+// Folds a tile: rows past the end of its shard (all but the last tile have none) become minus
+// infinity, 2^x of which is 0, so that one loop without masks serves both.
+template <class G, bool TOP>
+__device__ __forceinline__ void fold_block(const ScoreArgs& a, f32x16_t (&acc)[G::MB][G::NB], int ti, int rows, int n0,
+                                           int wm, int wn, int lane, Fold (&f)[G::NB]) {
+  const bool full = rows == G::BM;
+  const int lim = rows - wm - 4 * (lane >> 5);
+  if (!full)
+#pragma unroll
+    for (int j = 0; j < G::NB; ++j)
+#pragma unroll
+      for (int i = 0; i < G::MB; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          acc[i][j][r] = 32 * i + 8 * (r >> 2) + (r & 3) < lim ? acc[i][j][r] : -INFINITY;
+#pragma unroll
+  for (int j = 0; j < G::NB; ++j) {
+    const int64_t n = n0 + wn + 32 * j + (lane & 31);
+    float *fine = nullptr, *coarse = nullptr;
+    if (TOP && n < a.f.T) {
+      fine = a.fine + ((int64_t)ti * a.f.T + n) * (G::BM / 4) + wm / 4;
+      coarse = a.coarse + ((int64_t)ti * a.f.T + n) * (2 * G::WGM) + wm / G::WM * 2 + (lane >> 5);
+    }
+    fold_score<G::MB, G::NB, TOP>(acc, j, full, lim, f[j], lane, fine, coarse);
+  }
+}
+
+// End of a workgroup: as write_partials of vpce_tiles.h, with the third plane.
+template <class G>
+__device__ __forceinline__ void write_folds(const ScoreArgs& a, Fold (&f)[G::NB], int split, int n0, float* red) {
+  constexpr int BN = G::BN, NB = G::NB;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = G::wave_n(wave);
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+    merge_fold(f[j], Fold{__shfl_xor(f[j].m, 32), __shfl_xor(f[j].s, 32), __shfl_xor(f[j].u, 32)});
+  __syncthreads();
+  const int wr = wave / G::WGN;  // red: [WGM][3][BN]
+  if (lane < 32) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      float* r = red + wr * 3 * BN + wn + 32 * j + lane;
+      r[0] = f[j].m;
+      r[BN] = f[j].s;
+      r[2 * BN] = f[j].u;
+    }
+  }
+  __syncthreads();
+  if (wr == 0 && lane < 32) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int c = wn + 32 * j + lane;
+      for (int w = 1; w < G::WGM; ++w) {
+        const float* r = red + w * 3 * BN + c;
+        merge_fold(f[j], Fold{r[0], r[BN], r[2 * BN]});
+      }
+      const int64_t n = n0 + c;
+      if (n < a.f.T) {
+        a.f.m_part[(int64_t)split * a.f.T + n] = f[j].m == kNoLogit ? -INFINITY : f[j].m;
+        a.f.s_part[(int64_t)split * a.f.T + n] = f[j].s;
+        a.u_part[(int64_t)split * a.f.T + n] = f[j].u;
+      }
+    }
+  }
+}
+
+// fwd_kernel of vpce_kernels.hip with the fold above.
+template <class E, class G, bool TOP>
+__global__ void __launch_bounds__(G::NT, G::OCC) score_kernel(ScoreArgs a) {
+  using S = typename E::storage;
+  constexpr int BM = G::BM, BN = G::BN, MB = G::MB, NB = G::NB;
+  constexpr int RING = G::LDS_ELEMS * (int)sizeof(S);
+  __shared__ __attribute__((aligned(16))) char smem[kIsF8<E> ? 160 * 1024 : RING];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = G::wave_m(wave), wn = G::wave_n(wave);
+  const int logical = xcd_logical(blockIdx.x, gridDim.x);
+  const int tb = logical / a.f.n_splits;
+  const int split = logical % a.f.n_splits;
+  const int n0 = tb * BN;
+  const int t_begin = (int)((int64_t)split * a.f.n_tiles / a.f.n_splits);
+  const int t_end = (int)((int64_t)(split + 1) * a.f.n_tiles / a.f.n_splits);
+
+  Fold f[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) f[j] = Fold{kNoLogit, 0.f, 0.f};
+  ScalesFor<E, G> sc;
+  if constexpr (kIsF8<E>) {
+    sc.h = (uint8_t*)smem + RING;
+    sc.w = sc.h + Scales<G>::H_BYTES;
+    sc.load_tokens(a, n0);
+  }
+  int pos = 0;
+  for (int ti = t_begin; ti < t_end; ++ti) {
+    while (ti >= a.f.st.tile0[pos + 1]) ++pos;
+    const int r0 = (ti - a.f.st.tile0[pos]) * BM;
+    const int rows = min(BM, a.f.st.rows[pos] - r0);
+    const S* Wt = (const S*)a.f.st.w[pos] + (int64_t)r0 * a.f.d;
+
+    f32x16_t acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = f32x16_t{};
+    if constexpr (kIsF8<E>) {
+      if (!sc.has(ti)) sc.load_tiles(a, ti, t_end);
+      G::run(acc, Wt, a.f.d, rows, (const S*)a.f.H, a.f.d, n0, (int)a.f.T, a.f.d, smem, sc, ti);
+    } else {
+      G::run(acc, Wt, a.f.d, 0, rows, (const S*)a.f.H, a.f.d, n0, (int)a.f.T, a.f.d, (S*)smem);
+    }
+    fold_block<G, TOP>(a, acc, ti, rows, n0, wm, wn, lane, f);
+  }
+  write_folds<G>(a, f, split, n0, (float*)smem);
+  if (blockIdx.x == 0 && tid == 0 && a.f.counter) *a.f.counter = 0ull;
+}
+
+// stream_fwd_kernel of vpce_kernels.hip with the fold above.
+template <class E, class G, bool TOP>
+__global__ void __launch_bounds__(G::NT, G::OCC* G::NWAVES / 4) score_stream_kernel(ScoreArgs a) {
+  using S = typename E::storage;
+  constexpr int BM = G::BM, BN = G::BN, MB = G::MB, NB = G::NB;
+  __shared__ __attribute__((aligned(16))) char smem[kIsF8<E> ? 160 * 1024 : G::LDS_BYTES];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = G::wave_m(wave), wn = G::wave_n(wave);
+  const int logical = xcd_logical(blockIdx.x, gridDim.x);
+  const int split = logical / a.f.n_tok_blocks;
+  const int n0 = (logical % a.f.n_tok_blocks) * BN;
+  const int t_begin = (int)((int64_t)split * a.f.n_tiles / a.f.n_splits);
+  const int t_end = (int)((int64_t)(split + 1) * a.f.n_tiles / a.f.n_splits);
+
+  Fold f[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) f[j] = Fold{kNoLogit, 0.f, 0.f};
+  ScalesFor<E, G> sc;
+  if constexpr (kIsF8<E>) {
+    sc.h = (uint8_t*)smem + G::LDS_BYTES;
+    sc.w = sc.h + Scales<G>::H_BYTES;
+    sc.load_tokens(a, n0);
+    sc.load_tiles(a, t_begin, t_end);
+  }
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  const int nk = (a.f.d + G::BK - 1) / G::BK;
+  const int tail_chunks = a.f.d % G::BK ? a.f.d % G::BK / E::VEC : G::CPR;
+  const int total = (t_end - t_begin) * nk;
+
+  const char* baseB = (const char*)((const S*)a.f.H + (int64_t)n0 * a.f.d);
+  const char* baseA = nullptr;
+  uint32_t offA[G::A_LOADS], offB[G::B_LOADS];
+  G::offsets(offB, (int)min((int64_t)BN, a.f.T - n0), a.f.d, wave, lane);
+  int l_pos = 0, l_tile = t_begin, l_kt = 0, l_slot = 0, loaded = 0;
+  auto load_next = [&]() {
+    if (l_kt == 0) {
+      while (l_tile >= a.f.st.tile0[l_pos + 1]) ++l_pos;
+      const int r0 = (l_tile - a.f.st.tile0[l_pos]) * BM;
+      baseA = (const char*)((const S*)a.f.st.w[l_pos] + (int64_t)r0 * a.f.d);
+      G::offsets(offA, min(BM, a.f.st.rows[l_pos] - r0), a.f.d, wave, lane);
+    }
+    const int chunks = l_kt == nk - 1 ? tail_chunks : G::CPR;
+    const uint32_t l = lds0 + (uint32_t)(l_slot * G::SLICE_BYTES);
+    G::issue(baseA + (int64_t)l_kt * 128, offA, chunks, l, wave, lane);
+    G::issue(baseB + (int64_t)l_kt * 128, offB, chunks, l + BM * 128, wave, lane);
+    if (++l_kt == nk) {
+      l_kt = 0;
+      ++l_tile;
+    }
+    l_slot = l_slot + 1 == G::STAGES ? 0 : l_slot + 1;
+    ++loaded;
+  };
+  for (int k = 0; k < min(G::STAGES - 1, total); ++k) load_next();
+
+  f32x16_t acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = f32x16_t{};
+  int pos = 0, ti = t_begin, kt = 0, slot = 0;
+  for (int it = 0; it < total; ++it) {  // (the waits of stream_fwd_kernel)
+    if (loaded - it == G::STAGES - 1)
+      wait_vmcnt<(G::STAGES - 2) * G::NLOADS>();
+    else
+      wait_vmcnt<0>();
+    wait_lgkmcnt0();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (loaded < total) load_next();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (kIsF8<E>) {
+      const int sa = sc.of_rows(ti, wm, kt);
+      int sb[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) sb[j] = sc.of_token(wn + 32 * j + (lane & 31), kt);
+      G::multiply(acc, smem + slot * G::SLICE_BYTES, wm, wn, lane, sa, sb);
+    } else {
+      G::multiply(acc, smem + slot * G::SLICE_BYTES, wm, wn, lane);
+    }
+    slot = slot + 1 == G::STAGES ? 0 : slot + 1;
+    if (++kt == nk) {
+      kt = 0;
+      while (ti >= a.f.st.tile0[pos + 1]) ++pos;
+      const int r0 = (ti - a.f.st.tile0[pos]) * BM;
+      const int rows = min(BM, a.f.st.rows[pos] - r0);
+      fold_block<G, TOP>(a, acc, ti, rows, n0, wm, wn, lane, f);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) acc[i][j] = f32x16_t{};
+      }
+      ++ti;
+      if constexpr (kIsF8<E>)
+        if (ti < t_end && !sc.has(ti)) sc.load_tiles(a, ti, t_end);
+    }
+  }
+  write_folds<G>(a, f, split, n0, (float*)smem);
+  if (blockIdx.x == 0 && tid == 0 && a.f.counter) *a.f.counter = 0ull;
+}
+
+// Operands in float64, where their products are exact: the N elements of 16 bytes.
+template <class E>
+struct Dot;
+template <>
+struct Dot<Bf16> {
+  static constexpr int N = 8;
+  __device__ static void unpack(uint4 u, double (&f)[N]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      f[2 * k] = (double)__uint_as_float(w[k] << 16);
+      f[2 * k + 1] = (double)__uint_as_float(w[k] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Dot<F32> {
+  static constexpr int N = 4;
+  __device__ static void unpack(uint4 u, double (&f)[N]) {
+    f[0] = (double)__uint_as_float(u.x);
+    f[1] = (double)__uint_as_float(u.y);
+    f[2] = (double)__uint_as_float(u.z);
+    f[3] = (double)__uint_as_float(u.w);
+  }
+};
+template <>
+struct Dot<F8> {
+  static constexpr int N = 16;
+  __device__ static void unpack(uint4 u, double (&f)[N]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false);
+      const f32x2_t hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
+      f[4 * k] = (double)lo[0];
+      f[4 * k + 1] = (double)lo[1];
+      f[4 * k + 2] = (double)hi[0];
+      f[4 * k + 3] = (double)hi[1];
+    }
+  }
+};
+__device__ __forceinline__ double pow2_byte(int b) {  // 2^(b - 127), NaN for 255
+  return b == 255 ? __builtin_nan("") : ldexp(1.0, b - 127);
+}
+
+// Joins the splits of every token, a wavefront each, and finishes it as comb_kernel of
+// vpce_kernels.hip does, with the entropy, which is NaN where lse is not finite.  The target's logit is
+// taken here, in float64, and not from the tile that has it: the matrix unit rounds an 8-bit
+// product's sum more coarsely than a float32 one (2e-5 of a logit, d = 4096), which lse averages over
+// the vocabulary and a single logit does not (loss off by 2.8e-6 relative with the tile's, 6e-8 so);
+// and a wave of the product's kernel keeps no targets in registers that it needs for operands.
+template <class E>
+__global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreArgs sa) {
+  using S = typename E::storage;
+  constexpr int N = Dot<E>::N;
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= a.c.T) return;
+  Fold f{-INFINITY, 0.f, 0.f};
+  for (int k = lane; k < a.c.n_splits; k += 64) {
+    const int64_t i = (int64_t)k * a.c.T + t;
+    merge_fold(f, Fold{a.c.m_part[i], a.c.s_part[i], a.u_part[i]});
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1)
+    merge_fold(f, Fold{__shfl_xor(f.m, o), __shfl_xor(f.s, o), __shfl_xor(f.u, o)});
+  const float log_s = __builtin_amdgcn_logf(f.s);
+  const float lse = (f.m + log_s) * kLn2;
+  const int64_t tg = a.c.targets[t];
+  double y = 0.0;
+  if (tg >= 0 && tg < a.c.V) {
+    const ShardTable& st = sa.f.st;
+    int pos = 0;
+    while (tg >= st.off[pos] + st.rows[pos]) ++pos;
+    const int64_t row = tg - st.off[pos];
+    const uint4* h = (const uint4*)((const S*)sa.f.H + t * sa.f.d);
+    const uint4* w = (const uint4*)((const S*)st.w[pos] + row * sa.f.d);
+#pragma unroll 2
+    for (int c = lane; c < sa.f.d / N; c += 64) {
+      double x[N], v[N], p = 0.0, scale = 1.0;
+      Dot<E>::unpack(h[c], x);
+      Dot<E>::unpack(w[c], v);
+      if constexpr (kIsF8<E>)
+        scale = pow2_byte(sa.h_scale[t * sa.nb + c / 8]) * pow2_byte(sa.w_scale[pos][row / 128 * sa.nb + c / 8]);
+#pragma unroll
+      for (int k = 0; k < N; ++k) p = fma(x[k], v[k], p);
+      y = fma(p, scale, y);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) y += __shfl_xor(y, o);
+  }
+  if (lane) return;
+  float loss;
+  if (tg == a.c.ignore_index) {
+    loss = 0.f;
+  } else if (tg < 0 || tg >= a.c.V) {
+    loss = __builtin_nanf("");
+    atomicAdd(a.c.bad_counter, 1ull);
+  } else {
+    loss = (float)((double)lse - y);
+  }
+  a.c.lse[t] = lse;
+  a.c.loss[t] = loss;
+  if (a.entropy) a.entropy[t] = (log_s - f.u / f.s) * kLn2;
+}
+
+// ---------------------------------------------------------------------------
+// The most likely ids of a token, one workgroup each.  Bound by latency: a few dependent reads of
+// maxima, then four rows of W for each group of ids that is looked at.
+constexpr int kTopThreads = 256, kExtra = 4, kMaxGroups = VP_MAX_TOP + kExtra;
+constexpr int kCoarseRoom = 512, kFineRoom = 1024;
+
+// The larger logit first, the lower id among equals.
+template <class V, class I>
+__device__ __forceinline__ bool before(V va, I ia, V vb, I ib) {
+  return va > vb || (va == vb && ia < ib);
+}
+
+template <class E>
+__global__ void __launch_bounds__(kTopThreads) top_kernel(TopArgs a) {
+  using S = typename E::storage;
+  constexpr int N = Dot<E>::N;
+  __shared__ float side[kTopThreads];
+  __shared__ float cand_v[kFineRoom];
+  __shared__ int cand_g[kFineRoom], list[kCoarseRoom];
+  __shared__ int sel[kMaxGroups], sel_pos[kMaxGroups], sel_row[kMaxGroups];
+  __shared__ double val[4 * kMaxGroups];
+  __shared__ int64_t gid[4 * kMaxGroups];
+  __shared__ int count[2];
+  __shared__ float tau_s;
+  __shared__ float best_v[kTopThreads / 64];
+  __shared__ int best_g[kTopThreads / 64];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const FwdArgs& f = a.s.f;
+  const int64_t T = f.T, t = xcd_logical(blockIdx.x, gridDim.x);
+  const float lse = a.lse[t];
+  int64_t* ids = a.ids + t * a.top;
+  float* loss = a.loss + t * a.top;
+  if (!(__builtin_fabsf(lse) < INFINITY)) {
+    if (tid < a.top) {
+      ids[tid] = -1;
+      loss[tid] = __builtin_nanf("");
+    }
+    return;
+  }
+  const int F = a.bm / 4, cpt = a.cpt, fpc = F / cpt, nc = f.n_tiles * cpt;
+  const int want = a.top + kExtra;
+  auto coarse = [&](int c) { return a.s.coarse[((int64_t)(c / cpt) * T + t) * cpt + c % cpt]; };
+  auto fine = [&](int g) { return a.s.fine[((int64_t)(g / F) * T + t) * F + g % F]; };
+
+  // tau: the want-th largest of the threads' maxima, which as many coarse maxima reach
+  float mine = -INFINITY;
+#pragma unroll 4
+  for (int c = tid; c < nc; c += kTopThreads) mine = fmaxf(mine, coarse(c));
+  side[tid] = mine;
+  if (tid < 2) count[tid] = 0;
+  __syncthreads();
+  int rank = 0;
+#pragma unroll 8
+  for (int k = 0; k < kTopThreads; ++k) rank += before(side[k], k, mine, tid);
+  if (rank == want - 1) tau_s = mine;
+  __syncthreads();
+  const float tau = tau_s;
+  if (mine >= tau)
+    for (int c = tid; c < nc; c += kTopThreads)
+      if (coarse(c) >= tau) {
+        const int k = atomicAdd(&count[0], 1);
+        if (k < kCoarseRoom) list[k] = c;
+      }
+  __syncthreads();
+  const int n_coarse = count[0];
+  if (n_coarse <= kCoarseRoom) {
+    for (int e = tid; e < n_coarse * fpc; e += kTopThreads) {
+      const int c = list[e / fpc], within = c % cpt;
+      const int g = c / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
+      const float v = fine(g);
+      if (v >= tau) {
+        const int k = atomicAdd(&count[1], 1);
+        if (k < kFineRoom) {
+          cand_v[k] = v;
+          cand_g[k] = g;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  int n = count[1], groups;
+  if (n_coarse <= kCoarseRoom && n <= kFineRoom) {
+    groups = min(n, want);
+    for (int e = tid; e < n; e += kTopThreads) {
+      const float v = cand_v[e];
+      const int g = cand_g[e];
+      int r = 0;
+      for (int k = 0; k < n; ++k) r += before(cand_v[k], cand_g[k], v, g);
+      if (r < want) sel[r] = g;
+    }
+  } else {
+    // Many equal logits: the groups one by one, each the next in order after the one before.
+    float last_v = INFINITY;
+    int last_g = -1;
+    groups = 0;
+    for (; groups < want; ++groups) {
+      float v = -INFINITY;
+      int g = INT32_MAX;
+      for (int k = tid; k < f.n_tiles * F; k += kTopThreads) {
+        const float x = fine(k);
+        if (x == x && before(last_v, last_g, x, k) && before(x, k, v, g)) {
+          v = x;
+          g = k;
+        }
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const float vo = __shfl_xor(v, o);
+        const int go = __shfl_xor(g, o);
+        if (before(vo, go, v, g)) {
+          v = vo;
+          g = go;
+        }
+      }
+      if (lane == 0) {
+        best_v[wave] = v;
+        best_g[wave] = g;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kTopThreads / 64; ++w)
+        if (before(best_v[w], best_g[w], v, g)) {
+          v = best_v[w];
+          g = best_g[w];
+        }
+      __syncthreads();
+      if (g == INT32_MAX) break;
+      if (tid == 0) sel[groups] = g;
+      last_v = v;
+      last_g = g;
+    }
+  }
+  __syncthreads();
+  if (tid < groups) {
+    const int g = sel[tid], tile = g / F;
+    int pos = 0;
+    while (tile >= f.st.tile0[pos + 1]) ++pos;
+    sel_pos[tid] = pos;
+    sel_row[tid] = (tile - f.st.tile0[pos]) * a.bm + g % F * 4;
+  }
+  __syncthreads();
+
+  const uint4* h = (const uint4*)((const S*)f.H + t * f.d);
+  const int chunks = f.d / N;
+  for (int s = wave; s < groups; s += kTopThreads / 64) {
+    const int pos = sel_pos[s], row = sel_row[s], live = min(4, f.st.rows[pos] - row);
+    const uint4* w = (const uint4*)((const S*)f.st.w[pos] + (int64_t)row * f.d);
+    double acc[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int c = lane; c < chunks; c += 64) {
+      double x[N], y[N];
+      uint4 raw[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) raw[r] = w[(int64_t)min(r, live - 1) * chunks + c];
+      Dot<E>::unpack(h[c], x);
+      double scale = 1.0;
+      if constexpr (kIsF8<E>) {
+        const int b = c / (128 / N);
+        scale = pow2_byte(a.s.h_scale[t * a.s.nb + b]) * pow2_byte(a.s.w_scale[pos][(int64_t)(row / 128) * a.s.nb + b]);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        Dot<E>::unpack(raw[r], y);
+        double p = 0.0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) p = fma(x[k], y[k], p);
+        acc[r] = fma(p, scale, acc[r]);
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[r] += __shfl_xor(acc[r], o);
+    if (lane < 4) {
+      const double v = lane == 0 ? acc[0] : lane == 1 ? acc[1] : lane == 2 ? acc[2] : acc[3];
+      val[4 * s + lane] = v;
+      gid[4 * s + lane] = lane < live ? f.st.off[pos] + row + lane : -1;
+    }
+  }
+  __syncthreads();
+  n = 4 * groups;
+  if (tid < n && gid[tid] >= 0) {
+    const double v = val[tid];
+    const int64_t g = gid[tid];
+    int r = 0;
+    for (int k = 0; k < n; ++k) r += gid[k] >= 0 && before(val[k], gid[k], v, g);
+    if (r < a.top) {
+      ids[r] = g;
+      loss[r] = (float)((double)lse - v);
+    }
+  }
+  // fewer ids than asked for
+  if (tid == 0) {
+    int live = 0;
+    for (int k = 0; k < n; ++k) live += gid[k] >= 0;
+    for (int k = live; k < a.top; ++k) {
+      ids[k] = -1;
+      loss[k] = INFINITY;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+template <class E, class G>
+static bool launch_score_g(const ScoreArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.f.n_tok_blocks * a.f.n_splits));
+  if (a.fine)
+    hipLaunchKernelGGL((score_kernel<E, G, true>), grid, dim3(G::NT), 0, s, a);
+  else
+    hipLaunchKernelGGL((score_kernel<E, G, false>), grid, dim3(G::NT), 0, s, a);
+  return launched_ok();
+}
+template <class E, class G>
+static bool launch_score_stream(const ScoreArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.f.n_tok_blocks * a.f.n_splits));
+  if (a.fine)
+    hipLaunchKernelGGL((score_stream_kernel<E, G, true>), grid, dim3(G::NT), 0, s, a);
+  else
+    hipLaunchKernelGGL((score_stream_kernel<E, G, false>), grid, dim3(G::NT), 0, s, a);
+  return launched_ok();
+}
+template <class E>
+static bool launch_score(const ScoreArgs& a, hipStream_t s) {
+  if (a.f.kind == 2) return launch_score_stream<E, typename Cfg<E>::Stream64>(a, s);
+  if constexpr (!kIsF8<E>)
+    if (a.f.kind == 1) return launch_score_stream<E, typename Cfg<E>::Stream128>(a, s);
+  if (a.f.d % E::KB == 0) return launch_score_g<E, typename Cfg<E>::Logits>(a, s);
+  return launch_score_g<E, typename Cfg<E>::LogitsTail>(a, s);
+}
+
+bool run_score(int dtype, const ScoreArgs& a, hipStream_t s) {
+  if (dtype == VP_E4M3) return launch_score<F8>(a, s);
+  return dtype == VP_BF16 ? launch_score<Bf16>(a, s) : launch_score<F32>(a, s);
+}
+
+template <class E>
+static bool launch_comb(const ScoreCombArgs& a, const ScoreArgs& sa, hipStream_t s) {
+  hipLaunchKernelGGL((score_comb_kernel<E>), dim3((unsigned)((a.c.T + 3) / 4)), dim3(256), 0, s, a, sa);
+  return launched_ok();
+}
+bool run_score_comb(int dtype, const ScoreCombArgs& a, const ScoreArgs& sa, hipStream_t s) {
+  if (dtype == VP_E4M3) return launch_comb<F8>(a, sa, s);
+  return dtype == VP_BF16 ? launch_comb<Bf16>(a, sa, s) : launch_comb<F32>(a, sa, s);
+}
+
+// Microseconds per 128-byte slice, as in fwd_tile_of of vpce_kernels.hip.
+FwdTile score_tile_f8(int kind) {
+  using G0 = GemmF8<false>;
+  if (kind == 0) return FwdTile{G0::BM, G0::BN, G0::OCC, 1.4, 1.8};
+  return FwdTile{RingF8::BM, RingF8::BN, RingF8::OCC, 0.47, 0.5};
+}
+
+int score_coarse(int kind) {
+  using C = Cfg<Bf16>;
+  static_assert(RingF8::WGM == C::Stream64::WGM && GemmF8<false>::WGM == C::Logits::WGM, "the types' tiles are alike");
+  return 2 * (kind == 0 ? C::Logits::WGM : kind == 1 ? C::Stream128::WGM : C::Stream64::WGM);
+}
+
+bool run_top(int dtype, const TopArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.s.f.T);
+  if (dtype == VP_E4M3)
+    hipLaunchKernelGGL(top_kernel<F8>, grid, dim3(kTopThreads), 0, s, a);
+  else if (dtype == VP_BF16)
+    hipLaunchKernelGGL(top_kernel<Bf16>, grid, dim3(kTopThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL(top_kernel<F32>, grid, dim3(kTopThreads), 0, s, a);
+  return launched_ok();
+}
+
+}  // namespace vpce

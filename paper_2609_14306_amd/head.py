@@ -39,6 +39,23 @@ class Norm:
         return _spec(f"X gamma {self._mean} rstd dY dX dgamma dbeta?", (x, x, f, f, f, f, f, f),
                      (Td, d, T, T, Td, Td, d, d))
 
+    @cached_property
+    def add_forward_spec(self):
+        import torch
+        f, x = torch.float32, _torch_dtype(self.c.dtype)
+        Td, d, T = (self.T, self.d), (self.d,), (self.T,)
+        return _spec(f"X R gamma beta? S Y? Y8? scale? {self._mean} rstd",
+                     (x, x, x, x, x, x, torch.float8_e4m3fn, torch.float8_e8m0fnu, f, f),
+                     (Td, Td, d, d, Td, Td, Td, (self.T, -(-self.d // 128)), T, T))
+
+    @cached_property
+    def add_backward_spec(self):
+        import torch
+        f, x = torch.float32, _torch_dtype(self.c.dtype)
+        Td, d, T = (self.T, self.d), (self.d,), (self.T,)
+        return _spec(f"S gamma {self._mean} rstd dY dS? dX dgamma dbeta?", (x, x, f, f, f, f, f, f, f),
+                     (Td, d, T, T, Td, Td, Td, d, d))
+
     @property
     def _mean(self):
         return "mean?" if self.rms else "mean"
@@ -193,6 +210,20 @@ def vp_norm_backward(norm: Norm, X, gamma, mean, rstd, dY, dX, dgamma, dbeta, ws
           ws, lambda: vp_norm_workspace_size(norm))
 
 
+def vp_add_norm_forward(norm: Norm, X, R, gamma, beta, S, Y, Y8, scale, mean, rstd, stream=None) -> None:
+    """S = X + R (S may be X or R) and the norm of it: Y, or Y8 with scale, or both; what is not wanted is
+    None, and so may be beta, and mean in the RMS form."""
+    _call("vp_add_norm_forward", (norm.ref,), norm.add_forward_spec, (X, R, gamma, beta, S, Y, Y8, scale, mean, rstd),
+          stream)
+
+
+def vp_add_norm_backward(norm: Norm, S, gamma, mean, rstd, dY, dS, dX, dgamma, dbeta, ws, stream=None) -> None:
+    """dX (which may be dY or dS), dgamma and dbeta (None: not computed); dS: the gradient that S has
+    elsewhere, or None."""
+    _call("vp_add_norm_backward", (norm.ref,), norm.add_backward_spec,
+          (S, gamma, mean, rstd, dY, dS, dX, dgamma, dbeta), stream, ws, lambda: vp_norm_workspace_size(norm))
+
+
 def vp_seq_workspace_size(seq: Sequences) -> int:
     """Bytes of the workspace of ``vp_pref_forward`` and ``vp_policy_forward``."""
     n = ctypes.c_size_t(0)
@@ -283,6 +314,33 @@ def layer_norm_backward(X, gamma, mean, rstd, dY, bias: bool = True, dX=None, dg
     dbeta = None if not bias else _f32(norm.d, like=X) if dbeta is None else dbeta
     ws = _bytes(vp_norm_workspace_size(norm), X) if ws is None else ws
     vp_norm_backward(norm, X, gamma, mean, rstd, dY, dX, dgamma, dbeta, ws)
+    return dX, dgamma, dbeta
+
+
+def add_norm(X, R, gamma, beta=None, eps: float = 1e-5, rms: bool = False, f8: bool = False):
+    """(S, Y, mean, rstd) with S = X + R [T, d] and Y its norm; mean is None in the RMS form.  With
+    `f8`, Y is (Y8, scale) as ``score_f8`` takes them."""
+    import torch
+    from .scoring import f8_buffers
+    norm = Norm(X.shape[0], X.shape[1], _dtype_code(X), eps, rms)
+    S, mean, rstd = torch.empty_like(X), None if rms else _f32(norm.T, like=X), _f32(norm.T, like=X)
+    Y8, scale = f8_buffers(norm.T, norm.d, 1, X.device) if f8 else (None, None)
+    Y = None if f8 else torch.empty_like(X)
+    vp_add_norm_forward(norm, X, R, gamma, beta, S, Y, Y8, scale, mean, rstd)
+    return S, (Y8, scale) if f8 else Y, mean, rstd
+
+
+def add_norm_backward(S, gamma, mean, rstd, dY, dS=None, bias: bool = True, dX=None, dgamma=None, dbeta=None,
+                      accumulate: bool = False, ws=None):
+    """(dX, dgamma, dbeta) float32: the gradient of X, which is that of R too, from dY and the gradient dS
+    that S has elsewhere; the rest as for ``layer_norm_backward``."""
+    _check_norm_grads(S, bias, dgamma, dbeta, accumulate)
+    norm = Norm(S.shape[0], S.shape[1], _dtype_code(S), 0.0, mean is None, accumulate)
+    dX = _f32(norm.T, norm.d, like=S) if dX is None else dX
+    dgamma = _f32(norm.d, like=S) if dgamma is None else dgamma
+    dbeta = None if not bias else _f32(norm.d, like=S) if dbeta is None else dbeta
+    ws = _bytes(vp_norm_workspace_size(norm), S) if ws is None else ws
+    vp_add_norm_backward(norm, S, gamma, mean, rstd, dY, dS, dX, dgamma, dbeta, ws)
     return dX, dgamma, dbeta
 
 
