@@ -940,7 +940,7 @@ ScorePlan score_plan(const vp_problem* p, int top) {
   s.off_s = s.off_m + plane;
   s.off_u = s.off_s + plane;
   s.off_fine = s.off_u + plane;
-  s.off_coarse = s.off_fine + (top > 0 ? align256((size_t)(s.Tc * rows)) : 0);
+  s.off_coarse = s.off_fine + (top > 0 ? align256((size_t)(round_up(s.Tc, 32) * rows)) : 0);
   s.total = s.off_coarse + (top > 0 ? align256((size_t)(s.Tc * (rows / 4))) : 0);
   return s;
 }
@@ -1013,8 +1013,7 @@ vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, con
     }
     if (!vpce::run_score(prob->dtype, a.s, s)) return VP_ERR_HIP;
 
-    vpce::ScoreCombArgs c;
-    memset(&c, 0, sizeof(c));
+    vpce::ScoreCombArgs& c = a.comb;
     c.c.m_part = f.m_part;
     c.c.s_part = f.s_part;
     c.c.targets = f.targets;
@@ -1027,11 +1026,13 @@ vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, con
     c.c.bad_counter = counter;
     c.u_part = a.s.u_part;
     c.entropy = entropy ? entropy + t0 : nullptr;
-    if (!vpce::run_score_comb(prob->dtype, c, a.s, s)) return VP_ERR_HIP;
-    if (top == 0) continue;
-    a.lse = c.c.lse;
+    if (top == 0) {
+      if (!vpce::run_score_comb(prob->dtype, c, a.s, s)) return VP_ERR_HIP;
+      continue;
+    }
     a.bm = ft.bm;
     a.cpt = vpce::score_coarse(fp.kind);
+    a.tok = vpce::score_tokens(fp.kind);
     a.top = top;
     a.ids = top_ids + t0 * top;
     a.loss = top_loss + t0 * top;

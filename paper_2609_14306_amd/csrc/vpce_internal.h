@@ -62,7 +62,9 @@ FwdTile fwd_tile(int dtype, int kind);
 struct ScoreArgs {
   FwdArgs f;
   float* u_part;  // [n_splits][T]: sum of 2^x x, x the exponent (below 0) in s_part's sum
-  float* fine;    // [n_tiles][T][bm / 4], NaN where no row is live; null without alternatives
+  // [n_tiles][ceil(T / tok)][bm / 4][tok] with `tok` tokens side by side (score_tokens), NaN where no
+  // row is live; null without alternatives
+  float* fine;
   float* coarse;  // [n_tiles][T][cpt]
   // 8-bit operands: scales of H [T][nb] and of each shard in the table's order [rows / 128][nb]
   const uint8_t* h_scale;
@@ -81,8 +83,8 @@ struct ScoreCombArgs {
 
 struct TopArgs {
   ScoreArgs s;
-  const float* lse;
-  int32_t bm, cpt, top;
+  ScoreCombArgs comb;  // the token is finished in the same launch
+  int32_t bm, cpt, tok, top;
   int64_t* ids;  // [T][top]
   float* loss;   // [T][top]
 };
@@ -234,6 +236,7 @@ bool run_fill_zero(float* p, int64_t n, hipStream_t s);
 bool run_fwd(int dtype, const FwdArgs& a, hipStream_t s);
 bool run_comb(const CombArgs& a, hipStream_t s);
 int score_coarse(int kind);  // coarse maxima of a tile
+int score_tokens(int kind);  // tokens side by side in the fine maxima
 FwdTile score_tile_f8(int kind);  // kinds 0 and 2
 bool run_score(int dtype, const ScoreArgs& a, hipStream_t s);
 bool run_score_comb(int dtype, const ScoreCombArgs& a, const ScoreArgs& sa, hipStream_t s);

@@ -8,11 +8,11 @@
 // a sum of two terms that are not negative: nothing cancels.
 //
 // Alternatives.  No logits are kept; the fold leaves the maximum of every four consecutive ids
-// (fine) and of the logits that a lane holds of a tile (coarse).  The K + 4 largest fine maxima,
+// (fine) and of the logits that a lane holds of a tile (coarse).  The K + 2 largest fine maxima,
 // ties by the lower ids, hold the K largest logits but for what float32 sums round: the logits of
 // those ids are taken again in float64, where the products of the operands are exact, and ranked by
-// that.  An answer differs from the float64 one only where five groups of ids lie within the
-// rounding of a float32 sum at its border.
+// that.  An answer differs from the float64 one only where three groups of ids lie within the
+// rounding of the sums at its border.
 //
 // 8-bit operands (e4m3) have a power of two as scale for every 128 columns of a token and every 128
 // x 128 block of a shard.  A slice of 128 bytes is one such block: the matrix instruction of
@@ -21,6 +21,7 @@
 #include <stdint.h>
 
 #include "vpce_internal.h"
+#include "vpce_lanes.h"
 #include "vpce_tiles.h"
 
 namespace vpce {
@@ -233,10 +234,17 @@ __device__ __forceinline__ void merge_fold(Fold& f, Fold o) {
   f.u += o.u;
 }
 
+// Tokens whose fine maxima lie side by side: on the large tiles the 32 of a column block, so that
+// every store fills whole lines of memory (T = 4096, V = 201088: the stores cost the product 1% and
+// the pieces of 16 bytes that a token alone has 3.7%), and one on the small ones, which have few
+// tokens (T = 1, V = 151936: 261 us in all, and 265 with 32).
+template <class G>
+constexpr int kFineTokens = G::SKIPS ? 32 : 1;
+
 // Folds column block j of a logits tile (fold_tile of vpce_tiles.h with the third sum) and, with
 // TOP, leaves its maxima: fine, the bm / 4 ones of this tile and the lane's token, and coarse
 // (both null for a token that does not exist).  Rows from `lim` on are minus infinity.
-template <int MB, int NB, bool TOP>
+template <int MB, int NB, bool TOP, int TOK>
 __device__ __forceinline__ void fold_score(const f32x16_t (&acc)[MB][NB], int j, bool full, int lim, Fold& f,
                                            int lane, float* fine, float* coarse) {
   float g[MB][4], top = -INFINITY;
@@ -257,18 +265,26 @@ __device__ __forceinline__ void fold_score(const f32x16_t (&acc)[MB][NB], int j,
       for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q) g[i][q] = 32 * i + 8 * q < lim ? g[i][q] : __builtin_nanf("");
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-      // The lanes l and l + 32 hold the even and the odd ones of the block's eight maxima; after
-      // two swaps of half wavefronts they hold the first and the last four.
-      typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
-      const u32x2_t x = __builtin_bit_cast(
-          u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(g[i][0]), __float_as_uint(g[i][2]), false, false));
-      const u32x2_t y = __builtin_bit_cast(
-          u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(g[i][1]), __float_as_uint(g[i][3]), false, false));
+    if constexpr (TOK == 32) {
       if (fine)
-        *(float4*)(fine + 8 * i + 4 * (lane >> 5)) =
-            make_float4(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(y[0]), __uint_as_float(y[1]));
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) fine[(8 * i + 2 * q + (lane >> 5)) * 32] = g[i][q];
+    } else {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        // The lanes l and l + 32 hold the even and the odd ones of the block's eight maxima; after
+        // two swaps of half wavefronts they hold the first and the last four.
+        typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+        const u32x2_t x = __builtin_bit_cast(
+            u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(g[i][0]), __float_as_uint(g[i][2]), false, false));
+        const u32x2_t y = __builtin_bit_cast(
+            u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(g[i][1]), __float_as_uint(g[i][3]), false, false));
+        if (fine)
+          *(float4*)(fine + 8 * i + 4 * (lane >> 5)) =
+              make_float4(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(y[0]), __uint_as_float(y[1]));
+      }
     }
   }
   const float tmax = top * kLog2e;
@@ -293,6 +309,7 @@ __device__ __forceinline__ void fold_score(const f32x16_t (&acc)[MB][NB], int j,
 template <class G, bool TOP>
 __device__ __forceinline__ void fold_block(const ScoreArgs& a, f32x16_t (&acc)[G::MB][G::NB], int ti, int rows, int n0,
                                            int wm, int wn, int lane, Fold (&f)[G::NB]) {
+  constexpr int TOK = kFineTokens<G>;
   const bool full = rows == G::BM;
   const int lim = rows - wm - 4 * (lane >> 5);
   if (!full)
@@ -308,10 +325,10 @@ __device__ __forceinline__ void fold_block(const ScoreArgs& a, f32x16_t (&acc)[G
     const int64_t n = n0 + wn + 32 * j + (lane & 31);
     float *fine = nullptr, *coarse = nullptr;
     if (TOP && n < a.f.T) {
-      fine = a.fine + ((int64_t)ti * a.f.T + n) * (G::BM / 4) + wm / 4;
+      fine = a.fine + (((int64_t)ti * ((a.f.T + TOK - 1) / TOK) + n / TOK) * (G::BM / 4) + wm / 4) * TOK + n % TOK;
       coarse = a.coarse + ((int64_t)ti * a.f.T + n) * (2 * G::WGM) + wm / G::WM * 2 + (lane >> 5);
     }
-    fold_score<G::MB, G::NB, TOP>(acc, j, full, lim, f[j], lane, fine, coarse);
+    fold_score<G::MB, G::NB, TOP, TOK>(acc, j, full, lim, f[j], lane, fine, coarse);
   }
 }
 
@@ -424,8 +441,6 @@ __global__ void __launch_bounds__(G::NT, G::OCC* G::NWAVES / 4) score_stream_ker
   if constexpr (kIsF8<E>) {
     sc.h = (uint8_t*)smem + G::LDS_BYTES;
     sc.w = sc.h + Scales<G>::H_BYTES;
-    sc.load_tokens(a, n0);
-    sc.load_tiles(a, t_begin, t_end);
   }
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
@@ -457,6 +472,10 @@ __global__ void __launch_bounds__(G::NT, G::OCC* G::NWAVES / 4) score_stream_ker
     ++loaded;
   };
   for (int k = 0; k < min(G::STAGES - 1, total); ++k) load_next();
+  if constexpr (kIsF8<E>) {  // (while the first slices are on their way)
+    sc.load_tokens(a, n0);
+    sc.load_tiles(a, t_begin, t_end);
+  }
 
   f32x16_t acc[MB][NB];
 #pragma unroll
@@ -551,20 +570,19 @@ __device__ __forceinline__ double pow2_byte(int b) {  // 2^(b - 127), NaN for 25
   return b == 255 ? __builtin_nan("") : ldexp(1.0, b - 127);
 }
 
-// Joins the splits of every token, a wavefront each, and finishes it as comb_kernel of
-// vpce_kernels.hip does, with the entropy, which is NaN where lse is not finite.  The target's logit is
-// taken here, in float64, and not from the tile that has it: the matrix unit rounds an 8-bit
-// product's sum more coarsely than a float32 one (2e-5 of a logit, d = 4096), which lse averages over
-// the vocabulary and a single logit does not (loss off by 2.8e-6 relative with the tile's, 6e-8 so);
-// and a wave of the product's kernel keeps no targets in registers that it needs for operands.
+// A wavefront finishes a token: joins its splits as comb_kernel of vpce_kernels.hip does, with the
+// entropy, which is NaN where lse is not finite; returns lse.  The target's logit is taken here, in
+// float64, and not from the tile that has it: the matrix unit rounds an 8-bit product's sum more
+// coarsely than a float32 one (2e-5 of a logit, d = 4096), which lse averages over the vocabulary and
+// a single logit does not (loss off by 2.8e-6 relative with the tile's, 6e-8 so); and a wave of the
+// product's kernel keeps no targets in registers that it needs for operands.
 template <class E>
-__global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreArgs sa) {
+__device__ __forceinline__ float finish_token(const ScoreCombArgs& a, const ScoreArgs& sa, int64_t t, int lane) {
   using S = typename E::storage;
   constexpr int N = Dot<E>::N;
-  const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= a.c.T) return;
+  const int64_t tg = a.c.targets[t];
   Fold f{-INFINITY, 0.f, 0.f};
+#pragma unroll 4
   for (int k = lane; k < a.c.n_splits; k += 64) {
     const int64_t i = (int64_t)k * a.c.T + t;
     merge_fold(f, Fold{a.c.m_part[i], a.c.s_part[i], a.u_part[i]});
@@ -574,16 +592,15 @@ __global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreA
     merge_fold(f, Fold{__shfl_xor(f.m, o), __shfl_xor(f.s, o), __shfl_xor(f.u, o)});
   const float log_s = __builtin_amdgcn_logf(f.s);
   const float lse = (f.m + log_s) * kLn2;
-  const int64_t tg = a.c.targets[t];
   double y = 0.0;
   if (tg >= 0 && tg < a.c.V) {
     const ShardTable& st = sa.f.st;
-    int pos = 0;
-    while (tg >= st.off[pos] + st.rows[pos]) ++pos;
+    const int64_t end = lane < st.P ? st.off[lane] + st.rows[lane] : INT64_MAX;  // a shard a lane
+    const int pos = __popcll(__ballot(end <= tg));
     const int64_t row = tg - st.off[pos];
     const uint4* h = (const uint4*)((const S*)sa.f.H + t * sa.f.d);
     const uint4* w = (const uint4*)((const S*)st.w[pos] + row * sa.f.d);
-#pragma unroll 2
+#pragma unroll 4
     for (int c = lane; c < sa.f.d / N; c += 64) {
       double x[N], v[N], p = 0.0, scale = 1.0;
       Dot<E>::unpack(h[c], x);
@@ -597,7 +614,7 @@ __global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreA
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) y += __shfl_xor(y, o);
   }
-  if (lane) return;
+  if (lane) return lse;
   float loss;
   if (tg == a.c.ignore_index) {
     loss = 0.f;
@@ -610,13 +627,23 @@ __global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreA
   a.c.lse[t] = lse;
   a.c.loss[t] = loss;
   if (a.entropy) a.entropy[t] = (log_s - f.u / f.s) * kLn2;
+  return lse;
+}
+
+template <class E>
+__global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreArgs sa) {
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t < a.c.T) finish_token<E>(a, sa, t, threadIdx.x & 63);
 }
 
 // ---------------------------------------------------------------------------
-// The most likely ids of a token, one workgroup each.  Bound by latency: a few dependent reads of
-// maxima, then four rows of W for each group of ids that is looked at.
-constexpr int kTopThreads = 256, kExtra = 4, kMaxGroups = VP_MAX_TOP + kExtra;
+// The most likely ids of a token, one workgroup of NT threads each, which finishes the token too.
+// Bound by latency for few tokens (a few dependent reads of maxima, then four rows of W for each group
+// of ids that is looked at; 16 wavefronts side by side), and for many by those rows: (K + 2) 4 d
+// elements a token.
+constexpr int kExtra = 2, kMaxGroups = VP_MAX_TOP + kExtra;
 constexpr int kCoarseRoom = 512, kFineRoom = 1024;
+constexpr int kKeep = 4;  // fours of coarse maxima that a thread keeps in registers
 
 // The larger logit first, the lower id among equals.
 template <class V, class I>
@@ -624,62 +651,82 @@ __device__ __forceinline__ bool before(V va, I ia, V vb, I ib) {
   return va > vb || (va == vb && ia < ib);
 }
 
-template <class E>
-__global__ void __launch_bounds__(kTopThreads) top_kernel(TopArgs a) {
+template <class E, int NT>
+__global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
   using S = typename E::storage;
-  constexpr int N = Dot<E>::N;
-  __shared__ float side[kTopThreads];
+  constexpr int N = Dot<E>::N, WAVES = NT / 64;
+  __shared__ float side[WAVES][64];
   __shared__ float cand_v[kFineRoom];
   __shared__ int cand_g[kFineRoom], list[kCoarseRoom];
-  __shared__ int sel[kMaxGroups], sel_pos[kMaxGroups], sel_row[kMaxGroups];
+  __shared__ int sel[kMaxGroups];
   __shared__ double val[4 * kMaxGroups];
   __shared__ int64_t gid[4 * kMaxGroups];
   __shared__ int count[2];
-  __shared__ float tau_s;
-  __shared__ float best_v[kTopThreads / 64];
-  __shared__ int best_g[kTopThreads / 64];
+  __shared__ float tau_s, lse_s;
+  __shared__ float best_v[WAVES];
+  __shared__ int best_g[WAVES];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const FwdArgs& f = a.s.f;
   const int64_t T = f.T, t = xcd_logical(blockIdx.x, gridDim.x);
-  const float lse = a.lse[t];
   int64_t* ids = a.ids + t * a.top;
   float* loss = a.loss + t * a.top;
-  if (!(__builtin_fabsf(lse) < INFINITY)) {
-    if (tid < a.top) {
-      ids[tid] = -1;
-      loss[tid] = __builtin_nanf("");
-    }
-    return;
-  }
-  const int F = a.bm / 4, cpt = a.cpt, fpc = F / cpt, nc = f.n_tiles * cpt;
+  const int F = a.bm / 4, cpt = a.cpt, fpc = F / cpt, n4 = f.n_tiles * (cpt / 4);
   const int want = a.top + kExtra;
-  auto coarse = [&](int c) { return a.s.coarse[((int64_t)(c / cpt) * T + t) * cpt + c % cpt]; };
-  auto fine = [&](int g) { return a.s.fine[((int64_t)(g / F) * T + t) * F + g % F]; };
+  // coarse maxima 4 c .. 4 c + 3, and fine maximum g of all tiles
+  const int per_tile = cpt / 4, shift = per_tile - 1;  // 1 or 2 fours a tile
+  auto coarse = [&](int c) {
+    return ((const float4*)a.s.coarse)[((int64_t)(c >> shift) * T + t) * per_tile + (c & shift)];
+  };
+  const int tok = a.tok;
+  const float* fine_t = a.s.fine + t / tok * F * tok + t % tok;
+  auto fine = [&](int g) { return fine_t[((int64_t)(g / F) * ((T + tok - 1) / tok) * F + g % F) * tok]; };
+  auto max4 = [](float4 v) { return fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)); };
 
-  // tau: the want-th largest of the threads' maxima, which as many coarse maxima reach
+  // tau: the want-th largest of 64 maxima over the threads' shares, which as many coarse maxima
+  // reach
+  const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+  float4 keep[kKeep];
   float mine = -INFINITY;
-#pragma unroll 4
-  for (int c = tid; c < nc; c += kTopThreads) mine = fmaxf(mine, coarse(c));
-  side[tid] = mine;
+#pragma unroll
+  for (int k = 0; k < kKeep; ++k) keep[k] = tid + k * NT < n4 ? coarse(tid + k * NT) : none;
+#pragma unroll
+  for (int k = 0; k < kKeep; ++k) mine = fmaxf(mine, max4(keep[k]));
+#pragma unroll 8
+  for (int c = tid + kKeep * NT; c < n4; c += NT) mine = fmaxf(mine, max4(coarse(c)));
+  side[wave][lane] = mine;
   if (tid < 2) count[tid] = 0;
   __syncthreads();
-  int rank = 0;
-#pragma unroll 8
-  for (int k = 0; k < kTopThreads; ++k) rank += before(side[k], k, mine, tid);
-  if (rank == want - 1) tau_s = mine;
+  if (wave == 0) {
+    float all = mine;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) all = fmaxf(all, side[w][lane]);
+    int rank = 0;
+#pragma unroll
+    for (int k = 0; k < 64; ++k) rank += before(lane_read(all, k), k, all, lane);
+    if (rank == want - 1) tau_s = all;
+  }
   __syncthreads();
   const float tau = tau_s;
-  if (mine >= tau)
-    for (int c = tid; c < nc; c += kTopThreads)
-      if (coarse(c) >= tau) {
+  auto take = [&](int c, float4 v) {
+    const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (x[j] >= tau) {
         const int k = atomicAdd(&count[0], 1);
-        if (k < kCoarseRoom) list[k] = c;
+        if (k < kCoarseRoom) list[k] = 4 * c + j;
       }
+  };
+  if (mine >= tau) {
+#pragma unroll
+    for (int k = 0; k < kKeep; ++k)
+      if (tid + k * NT < n4) take(tid + k * NT, keep[k]);
+    for (int c = tid + kKeep * NT; c < n4; c += NT) take(c, coarse(c));
+  }
   __syncthreads();
   const int n_coarse = count[0];
   if (n_coarse <= kCoarseRoom) {
-    for (int e = tid; e < n_coarse * fpc; e += kTopThreads) {
+    for (int e = tid; e < n_coarse * fpc; e += NT) {
       const int c = list[e / fpc], within = c % cpt;
       const int g = c / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
       const float v = fine(g);
@@ -696,7 +743,7 @@ __global__ void __launch_bounds__(kTopThreads) top_kernel(TopArgs a) {
   int n = count[1], groups;
   if (n_coarse <= kCoarseRoom && n <= kFineRoom) {
     groups = min(n, want);
-    for (int e = tid; e < n; e += kTopThreads) {
+    for (int e = tid; e < n; e += NT) {
       const float v = cand_v[e];
       const int g = cand_g[e];
       int r = 0;
@@ -711,7 +758,7 @@ __global__ void __launch_bounds__(kTopThreads) top_kernel(TopArgs a) {
     for (; groups < want; ++groups) {
       float v = -INFINITY;
       int g = INT32_MAX;
-      for (int k = tid; k < f.n_tiles * F; k += kTopThreads) {
+      for (int k = tid; k < f.n_tiles * F; k += NT) {
         const float x = fine(k);
         if (x == x && before(last_v, last_g, x, k) && before(x, k, v, g)) {
           v = x;
@@ -733,7 +780,7 @@ __global__ void __launch_bounds__(kTopThreads) top_kernel(TopArgs a) {
       }
       __syncthreads();
 #pragma unroll
-      for (int w = 0; w < kTopThreads / 64; ++w)
+      for (int w = 0; w < WAVES; ++w)
         if (before(best_v[w], best_g[w], v, g)) {
           v = best_v[w];
           g = best_g[w];
@@ -746,21 +793,19 @@ __global__ void __launch_bounds__(kTopThreads) top_kernel(TopArgs a) {
     }
   }
   __syncthreads();
-  if (tid < groups) {
-    const int g = sel[tid], tile = g / F;
-    int pos = 0;
-    while (tile >= f.st.tile0[pos + 1]) ++pos;
-    sel_pos[tid] = pos;
-    sel_row[tid] = (tile - f.st.tile0[pos]) * a.bm + g % F * 4;
-  }
-  __syncthreads();
-
   const uint4* h = (const uint4*)((const S*)f.H + t * f.d);
   const int chunks = f.d / N;
-  for (int s = wave; s < groups; s += kTopThreads / 64) {
-    const int pos = sel_pos[s], row = sel_row[s], live = min(4, f.st.rows[pos] - row);
+  if (wave == 0) {
+    const float lse = finish_token<E>(a.comb, a.s, t, lane);
+    if (lane == 0) lse_s = lse;
+  }
+  for (int s = wave - 1; s < groups && wave > 0; s += WAVES - 1) {
+    const int g = __builtin_amdgcn_readfirstlane(sel[s]), tile = g / F;
+    const int pos = __popcll(__ballot(f.st.tile0[lane + 1] <= tile));  // (a shard a lane)
+    const int row = (tile - f.st.tile0[pos]) * a.bm + g % F * 4, live = min(4, f.st.rows[pos] - row);
     const uint4* w = (const uint4*)((const S*)f.st.w[pos] + (int64_t)row * f.d);
     double acc[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 2
     for (int c = lane; c < chunks; c += 64) {
       double x[N], y[N];
       uint4 raw[4];
@@ -792,6 +837,14 @@ __global__ void __launch_bounds__(kTopThreads) top_kernel(TopArgs a) {
     }
   }
   __syncthreads();
+  const float lse = lse_s;
+  if (!(__builtin_fabsf(lse) < INFINITY)) {
+    if (tid < a.top) {
+      ids[tid] = -1;
+      loss[tid] = __builtin_nanf("");
+    }
+    return;
+  }
   n = 4 * groups;
   if (tid < n && gid[tid] >= 0) {
     const double v = val[tid];
@@ -870,15 +923,27 @@ int score_coarse(int kind) {
   return 2 * (kind == 0 ? C::Logits::WGM : kind == 1 ? C::Stream128::WGM : C::Stream64::WGM);
 }
 
-bool run_top(int dtype, const TopArgs& a, hipStream_t s) {
+// Up to 512 tokens, two workgroups of 1024 a CU, the latency of a token counts.
+template <class E>
+static bool launch_top(const TopArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.s.f.T);
-  if (dtype == VP_E4M3)
-    hipLaunchKernelGGL(top_kernel<F8>, grid, dim3(kTopThreads), 0, s, a);
-  else if (dtype == VP_BF16)
-    hipLaunchKernelGGL(top_kernel<Bf16>, grid, dim3(kTopThreads), 0, s, a);
+  if (a.s.f.T <= 512)
+    hipLaunchKernelGGL((top_kernel<E, 1024>), grid, dim3(1024), 0, s, a);
   else
-    hipLaunchKernelGGL(top_kernel<F32>, grid, dim3(kTopThreads), 0, s, a);
+    hipLaunchKernelGGL((top_kernel<E, 256>), grid, dim3(256), 0, s, a);
   return launched_ok();
+}
+int score_tokens(int kind) {
+  using C = Cfg<Bf16>;
+  static_assert(kFineTokens<GemmF8<false>> == kFineTokens<C::Logits> && kFineTokens<RingF8> == kFineTokens<C::Stream64> &&
+                    kFineTokens<C::Stream128> == kFineTokens<C::Stream64>,
+                "by the kind of tile alone");
+  return kind == 0 ? kFineTokens<C::Logits> : kFineTokens<C::Stream64>;
+}
+
+bool run_top(int dtype, const TopArgs& a, hipStream_t s) {
+  if (dtype == VP_E4M3) return launch_top<F8>(a, s);
+  return dtype == VP_BF16 ? launch_top<Bf16>(a, s) : launch_top<F32>(a, s);
 }
 
 }  // namespace vpce
