@@ -259,7 +259,8 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(
     for (int j = 0; j < VEC; ++j) dg[k][j] = db[k][j] = 0.f;
   }
   uint4 xn[NV];
-  float4 dyn[NV][VEC / 4], dsn[ADD ? NV : 1][VEC / 4];
+  // (dS of the next row, too; without AHEAD it is read where it is added)
+  float4 dyn[NV][VEC / 4], dsn[ADD && AHEAD ? NV : 1][VEC / 4];
   float mean_n = 0.f, rstd_n = 0.f;
   auto load = [&](int64_t t) {
     if (t >= a.T) return;
@@ -273,7 +274,7 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(
 #pragma unroll
         for (int q = 0; q < VEC / 4; ++q) {
           dyn[k][q] = dy[i * (VEC / 4) + q];
-          if constexpr (ADD) dsn[k][q] = ((const float4*)a.dS + t * (a.d / 4))[i * (VEC / 4) + q];
+          if constexpr (ADD && AHEAD) dsn[k][q] = ((const float4*)a.dS + t * (a.d / 4))[i * (VEC / 4) + q];
         }
       }
     }
@@ -286,14 +287,14 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(
     if (!AHEAD) load(t);
     uint4 xr[NV];
     float dy[NV][VEC];
-    float4 ds[ADD ? NV : 1][VEC / 4];
+    float4 ds[ADD && AHEAD ? NV : 1][VEC / 4];
     const float mean = mean_n, rstd = rstd_n;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       xr[k] = xn[k];
 #pragma unroll
       for (int q = 0; q < VEC / 4; ++q) {
-        if constexpr (ADD) ds[k][q] = dsn[k][q];
+        if constexpr (ADD && AHEAD) ds[k][q] = dsn[k][q];
         dy[k][4 * q] = dyn[k][q].x;
         dy[k][4 * q + 1] = dyn[k][q].y;
         dy[k][4 * q + 2] = dyn[k][q].z;
@@ -331,8 +332,17 @@ __global__ void __launch_bounds__((Row<E, LANES, EL>::NT)) norm_backward_kernel(
         for (int j = 0; j < VEC; ++j) {
           const float xh = (x[j] - mean) * rstd;
           g[j] = rstd * (g[j] * dy[k][j] - c1 - xh * c2);
-          if constexpr (ADD) g[j] += ((const float*)&ds[k][j / 4])[j % 4];
+          if constexpr (ADD && AHEAD) g[j] += ((const float*)&ds[k][j / 4])[j % 4];
         }
+        if constexpr (ADD && !AHEAD)
+#pragma unroll
+          for (int q = 0; q < VEC / 4; ++q) {
+            const float4 s4 = ((const float4*)a.dS + t * (a.d / 4))[i * (VEC / 4) + q];
+            g[4 * q] += s4.x;
+            g[4 * q + 1] += s4.y;
+            g[4 * q + 2] += s4.z;
+            g[4 * q + 3] += s4.w;
+          }
 #pragma unroll
         for (int q = 0; q < VEC / 4; ++q)
           dx[i * (VEC / 4) + q] = make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]);
@@ -422,7 +432,10 @@ bool launched_ok() { return hipGetLastError() == hipSuccess; }
 //   T = 16384, d = 7168: 256 x 32 5240 / 5480, 512 x 16 5330 / 5790, 1024 x 8 4440 / 5880
 // With few rows fewer bytes a lane win (bfloat16, d = 4096, 128 x 32 and 256 x 16: T = 1 3.2 and
 // 2.7 us, T = 512 4.3 and 3.8; T = 4096, which the cache holds, 12.6 and 13.5).
-template <class E, class F>
+// With a residual there are four streams instead of two, and 256 x 16 takes the widths of 128 x 32
+// (T = 32768, d = 2880, bfloat16: 116 us instead of 126 with the result in 8 bits, 128 instead of 135
+// without; the other layouts stay the fastest ones or within 2%).
+template <class E, bool ADD, class F>
 bool forward_layout(int d, F&& f) {
   if (d <= 64) return f.template run<8, 8>();
   if (d <= 128) return f.template run<16, 8>();
@@ -431,7 +444,7 @@ bool forward_layout(int d, F&& f) {
   if constexpr (E::VEC == 8) {
     if (d <= 1024) return f.template run<64, 16>();
     if (d <= 2048) return f.template run<128, 16>();
-    if (d <= 3456) return f.template run<128, 32>();
+    if (!ADD && d <= 3456) return f.template run<128, 32>();
     if (d <= 4096) return f.template run<256, 16>();
     if (d <= 8192) return f.template run<512, 16>();
   } else {
@@ -536,8 +549,8 @@ int norm_parts(int64_t T, int d) {
 
 template <bool RMS, bool ADD>
 static bool forward_of(int dtype, const NormArgs& a, hipStream_t s) {
-  return dtype == VP_BF16 ? forward_layout<Half>(a.d, Forward<Half, RMS, ADD>{a, s})
-                          : forward_layout<Single>(a.d, Forward<Single, RMS, ADD>{a, s});
+  return dtype == VP_BF16 ? forward_layout<Half, ADD>(a.d, Forward<Half, RMS, ADD>{a, s})
+                          : forward_layout<Single, ADD>(a.d, Forward<Single, RMS, ADD>{a, s});
 }
 bool run_norm_forward(int dtype, bool rms, const NormArgs& a, hipStream_t s) {
   if (a.R) return rms ? forward_of<true, true>(dtype, a, s) : forward_of<false, true>(dtype, a, s);
