@@ -711,29 +711,32 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
   }
   __syncthreads();
   const float tau = tau_s;
-  auto take = [&](int c, float4 v) {
-    const float x[4] = {v.x, v.y, v.z, v.w};
+  // The fine maxima that reach tau, or with `above` lie above it, among cand_*; whether they fit.
+  auto collect = [&](bool above) {
+    auto in = [&](float x) { return above ? x > tau : x >= tau; };
+    auto take = [&](int c, float4 v) {
+      const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (x[j] >= tau) {
-        const int k = atomicAdd(&count[0], 1);
-        if (k < kCoarseRoom) list[k] = 4 * c + j;
-      }
-  };
-  if (mine >= tau) {
+      for (int j = 0; j < 4; ++j)
+        if (in(x[j])) {
+          const int k = atomicAdd(&count[0], 1);
+          if (k < kCoarseRoom) list[k] = 4 * c + j;
+        }
+    };
+    if (in(mine)) {
 #pragma unroll
-    for (int k = 0; k < kKeep; ++k)
-      if (tid + k * NT < n4) take(tid + k * NT, keep[k]);
-    for (int c = tid + kKeep * NT; c < n4; c += NT) take(c, coarse(c));
-  }
-  __syncthreads();
-  const int n_coarse = count[0];
-  if (n_coarse <= kCoarseRoom) {
+      for (int k = 0; k < kKeep; ++k)
+        if (tid + k * NT < n4) take(tid + k * NT, keep[k]);
+      for (int c = tid + kKeep * NT; c < n4; c += NT) take(c, coarse(c));
+    }
+    __syncthreads();
+    const int n_coarse = count[0];
+    if (n_coarse > kCoarseRoom) return false;
     for (int e = tid; e < n_coarse * fpc; e += NT) {
       const int c = list[e / fpc], within = c % cpt;
       const int g = c / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
       const float v = fine(g);
-      if (v >= tau) {
+      if (in(v)) {
         const int k = atomicAdd(&count[1], 1);
         if (k < kFineRoom) {
           cand_v[k] = v;
@@ -741,10 +744,21 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
         }
       }
     }
+    __syncthreads();
+    return count[1] <= kFineRoom;
+  };
+  int groups = 0;
+  bool fits = collect(false), tied = false;
+  if (!fits) {
+    // Many logits equal tau (a token of zeros has nothing else): those above it, and of the equal
+    // ones the first.
+    __syncthreads();
+    if (tid < 2) count[tid] = 0;
+    __syncthreads();
+    tied = fits = collect(true);
   }
-  __syncthreads();
-  int n = count[1], groups;
-  if (n_coarse <= kCoarseRoom && n <= kFineRoom) {
+  int n = count[1];
+  if (fits) {
     groups = min(n, want);
     for (int e = tid; e < n; e += NT) {
       const float v = cand_v[e];
@@ -753,11 +767,26 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
       for (int k = 0; k < n; ++k) r += before(cand_v[k], cand_g[k], v, g);
       if (r < want) sel[r] = g;
     }
+    for (int base = 0; tied && groups < want && base < f.n_tiles * F; base += NT) {
+      const int g = base + tid;
+      const uint64_t hit = __ballot(g < f.n_tiles * F && fine(min(g, f.n_tiles * F - 1)) == tau);
+      if (lane == 0) best_g[wave] = __popcll(hit);
+      __syncthreads();
+      int at = groups + __popcll(hit & ((1ull << lane) - 1));
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        at += w < wave ? best_g[w] : 0;
+        groups += best_g[w];
+      }
+      if (hit >> lane & 1 && at < want) sel[at] = g;
+      __syncthreads();
+    }
+    groups = min(groups, want);
   } else {
-    // Many equal logits: the groups one by one, each the next in order after the one before.
+    // More above tau than there is room for (they lie in few threads' shares): the groups one by one,
+    // each the next in order after the one before.
     float last_v = INFINITY;
     int last_g = -1;
-    groups = 0;
     for (; groups < want; ++groups) {
       float v = -INFINITY;
       int g = INT32_MAX;

@@ -132,6 +132,8 @@ def test_extreme_scales():
     Ws[0].view(torch.uint8)[:, 1] -= 60
     Hs.view(torch.uint8)[:, 2] -= 100
     Ws[0].view(torch.uint8)[:, 2] += 101
+    Hs.view(torch.uint8)[:, 3], Ws[0].view(torch.uint8)[:, 3] = 0, 250  # 2^-127 and 2^123
+    Hs.view(torch.uint8)[5, 3], Hs.view(torch.uint8)[6, 3] = 4, 8
     ops = (H, Hs, W, Ws, t)
     check_f8(*ops, vp.score_f8(*ops, top=4), 4)
 

@@ -107,6 +107,34 @@ def test_equal_logits_go_to_the_lowest_ids(T, V):
     assert torch.equal(out[3], torch.cat([first, torch.arange(100, 126, device="cuda")]).expand(T, 32))
 
 
+@pytest.mark.parametrize("T, V", [(3, 151936), (700, 30000)])
+def test_tokens_of_zeros_and_few_distinct_logits(T, V):
+    """Padding tokens (all logits 0) among others, and vocabularies with long runs of equal rows above,
+    at and below the border."""
+    H, W, t = make("bf16", T, 64, [V // 2, V - V // 2])
+    H[::2] = 0.0
+    check(H, W, t, vp.score(H, W, t, top=20), 20)
+    for lo, hi, k in [(100, 20000, 3.0), (V // 2 - 60, V // 2, 5.0), (V // 2 - 3000, V // 2 - 2999, 9.0)]:
+        W[0][lo:hi] = 0.0
+        W[0][lo:hi, 0] = k
+    H[:, 0] = 1.0
+    check(H, W, t, vp.score(H, W, t, top=32), 32)
+
+
+def test_large_logits_in_few_shares():
+    """More logits above the first threshold than the lists take: every 64th tile's are large."""
+    V = 64 * 1024
+    H = torch.randn(600, 64, device="cuda")
+    H[:, 0] = 40.0
+    W = torch.randn(V, 64, device="cuda") / 8
+    for tile in (128, 256):
+        w = W.clone()
+        w[:, 0] = (torch.arange(V, device="cuda") // tile % 64 < 3).float()
+        t = torch.zeros(600, dtype=torch.int64, device="cuda")
+        check(H, [w], t, vp.score(H, [w], t, top=8), 8)
+        check(H[:9], [w], t[:9], vp.score(H[:9], [w], t[:9], top=8), 8)
+
+
 def test_repeated_rows():
     """The same row under several ids, in several shards: the lower id first."""
     H, W, t = make("bf16", 300, 256, [600, 700, 800])
