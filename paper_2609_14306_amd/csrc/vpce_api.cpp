@@ -934,13 +934,14 @@ ScorePlan score_plan(const vp_problem* p, int top) {
     const int64_t most = std::max<int64_t>(256, round_down(kTopBytes / (rows + rows / 4), 256));
     if (p->T > most) s.Tc = round_up(ceil_div(p->T, ceil_div(p->T, most)), 256);
   }
+  // Partial states for as many splits as the few tokens' tiles can take: partial_slots goes by the
+  // bytes of H, of which 8-bit rows have few (T = 40, d = 4096, V = 151936: 204 splits 135 us, 240 117).
   vp_problem part = *p;
-  part.T = s.Tc;
-  s.slots = partial_slots(&part);
-  if (s.Tc > 0) {
-    part.T = p->T % s.Tc;
-    s.slots = std::max(s.slots, partial_slots(&part));
-  }
+  auto slots = [&](int64_t T) {
+    part.T = T;
+    return std::max(partial_slots(&part), T <= kFewTokens ? 2 * kCUs * T : 0);
+  };
+  s.slots = std::max(slots(s.Tc), s.Tc > 0 ? slots(p->T % s.Tc) : 0);
   const size_t plane = align256((size_t)s.slots * 4);
   s.off_m = kHeaderBytes;
   s.off_s = s.off_m + plane;
