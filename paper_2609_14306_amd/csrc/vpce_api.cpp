@@ -129,7 +129,7 @@ int64_t count_tiles(const vp_problem* p, int bm) {
 struct FwdPlan {
   int kind, splits;
 };
-FwdPlan plan_fwd(const vp_problem* p, int64_t slots) {
+FwdPlan plan_fwd(const vp_problem* p, int64_t slots, vpce::FwdTile (*tile)(int, int) = vpce::fwd_tile) {
   FwdPlan best{0, splits_for(p)};
   if (p->T > kFewTokens) {
     // Whole tiles on the 256 x 256 tile again: where splits_for's workgroups leave a last
@@ -141,7 +141,7 @@ FwdPlan plan_fwd(const vp_problem* p, int64_t slots) {
     // the fastest (ms, panels in MiB): bf16 T = 38494, d = 6912, V = 142765, 8 splits 64.8
     // (108), 6 70.9 (145), 5 63.9 (176); bf16 T = 58208, d = 7104, V = 11195, 8 splits 8.1
     // (111), 4 7.9 (222); f32 T = 25549, d = 5696, V = 25891, 16 splits 63.6 (89), 5 59.1 (289).
-    const vpce::FwdTile t = vpce::fwd_tile(p->dtype, 0);
+    const vpce::FwdTile t = tile(p->dtype, 0);
     const int64_t blocks = ceil_div(p->T, t.bn), tiles = std::max<int64_t>(1, count_tiles(p, t.bm));
     auto turns = [&](int64_t S) { return ceil_div(tiles, S) * ceil_div(blocks * S, kCUs); };
     const int64_t base = turns(best.splits);
@@ -158,7 +158,7 @@ FwdPlan plan_fwd(const vp_problem* p, int64_t slots) {
   double best_time = 0;
   for (int kind = 0; kind < vpce::kFwdKinds; ++kind) {
     if (kind == 1 && p->dtype == VP_E4M3) continue;  // (not built)
-    const vpce::FwdTile t = vpce::fwd_tile(p->dtype, kind);
+    const vpce::FwdTile t = tile(p->dtype, kind);
     const int64_t blocks = ceil_div(p->T, t.bn), places = kCUs * t.per_cu;
     const int64_t tiles = std::max<int64_t>(1, count_tiles(p, t.bm));
     int64_t S = std::max<int64_t>(1, std::min(std::min(slots / p->T, places / blocks), tiles));
@@ -992,8 +992,8 @@ vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, con
   char* base = (char*)ws;
   for (int64_t t0 = 0; t0 < prob->T; t0 += plan.Tc) {
     const int64_t T = part.T = std::min(plan.Tc, prob->T - t0);
-    const FwdPlan fp = plan_fwd(&part, plan.slots);
-    const vpce::FwdTile ft = vpce::fwd_tile(prob->dtype, fp.kind);
+    const FwdPlan fp = plan_fwd(&part, plan.slots, vpce::score_tile);
+    const vpce::FwdTile ft = vpce::score_tile(prob->dtype, fp.kind);
     vpce::TopArgs a;
     memset(&a, 0, sizeof(a));
     vpce::FwdArgs& f = a.s.f;
@@ -1038,8 +1038,8 @@ vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, con
       continue;
     }
     a.bm = ft.bm;
-    a.cpt = vpce::score_coarse(fp.kind);
-    a.tok = vpce::score_tokens(fp.kind);
+    a.cpt = vpce::score_coarse(prob->dtype, fp.kind);
+    a.tok = vpce::score_tokens(prob->dtype, fp.kind);
     a.top = top;
     a.ids = top_ids + t0 * top;
     a.loss = top_loss + t0 * top;

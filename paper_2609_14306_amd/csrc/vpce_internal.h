@@ -235,9 +235,9 @@ bool run_ws_init(unsigned long long* counter, hipStream_t s);
 bool run_fill_zero(float* p, int64_t n, hipStream_t s);
 bool run_fwd(int dtype, const FwdArgs& a, hipStream_t s);
 bool run_comb(const CombArgs& a, hipStream_t s);
-int score_coarse(int kind);  // coarse maxima of a tile
-int score_tokens(int kind);  // tokens side by side in the fine maxima
-FwdTile score_tile_f8(int kind);  // kinds 0 and 2
+int score_coarse(int dtype, int kind);  // coarse maxima of a tile
+int score_tokens(int dtype, int kind);  // tokens side by side in the fine maxima
+FwdTile score_tile(int dtype, int kind);  // fwd_tile of the scoring kernels
 bool run_score(int dtype, const ScoreArgs& a, hipStream_t s);
 bool run_score_comb(int dtype, const ScoreCombArgs& a, const ScoreArgs& sa, hipStream_t s);
 bool run_top(int dtype, const TopArgs& a, hipStream_t s);

@@ -511,7 +511,6 @@ static FwdTile fwd_tile_of(int kind) {
   return b16 ? FwdTile{G0::BM, G0::BN, G0::OCC, 1.4, 1.8} : FwdTile{G0::BM, G0::BN, G0::OCC, 7.45, 7.45};
 }
 FwdTile fwd_tile(int dtype, int kind) {
-  if (dtype == VP_E4M3) return score_tile_f8(kind);
   return dtype == 1 ? fwd_tile_of<Bf16>(kind) : fwd_tile_of<F32>(kind);
 }
 

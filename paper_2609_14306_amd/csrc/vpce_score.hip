@@ -918,12 +918,34 @@ static bool launch_score_stream(const ScoreArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((score_stream_kernel<E, G, false>), grid, dim3(G::NT), 0, s, a);
   return launched_ok();
 }
+// The tiles of the forward, but for float32's middle one: the 128 x 128 tile of its backward, of
+// which two workgroups share a CU, reaches 136 TFLOP/s against the streamed one's 121 and the large
+// one's 144 (d = 2880, V = 50000, microseconds: T = 128 386 -> 375, T = 384 1163 -> 1073, T = 1024
+// 2629 -> 2492; d = 1000, V = 32003: T = 1333 806 -> 792, T = 1536 976 -> 905).
+template <class E> struct ScoreCfg {
+  using Large = typename Cfg<E>::Logits;
+  using Small = typename Cfg<E>::Stream64;
+  using Middle = typename Cfg<E>::Stream128;
+};
+template <> struct ScoreCfg<F8> {
+  using Large = GemmF8<false>;
+  using Small = RingF8;
+  using Middle = Small;  // (not built)
+};
+template <> struct ScoreCfg<F32> {
+  using Large = Cfg<F32>::Logits;
+  using Small = Cfg<F32>::Stream64;
+  using Middle = Cfg<F32>::Res128;
+};
 template <class E>
 static bool launch_score(const ScoreArgs& a, hipStream_t s) {
-  if (a.f.kind == 2) return launch_score_stream<E, typename Cfg<E>::Stream64>(a, s);
-  if constexpr (!kIsF8<E>)
-    if (a.f.kind == 1) return launch_score_stream<E, typename Cfg<E>::Stream128>(a, s);
-  if (a.f.d % E::KB == 0) return launch_score_g<E, typename Cfg<E>::Logits>(a, s);
+  using C = ScoreCfg<E>;
+  if (a.f.kind == 2) return launch_score_stream<E, typename C::Small>(a, s);
+  if constexpr (sizeof(typename E::storage) == 2)
+    if (a.f.kind == 1) return launch_score_stream<E, typename C::Middle>(a, s);
+  if constexpr (sizeof(typename E::storage) == 4)
+    if (a.f.kind == 1) return launch_score_g<E, typename C::Middle>(a, s);
+  if (a.f.d % E::KB == 0) return launch_score_g<E, typename C::Large>(a, s);
   return launch_score_g<E, typename Cfg<E>::LogitsTail>(a, s);
 }
 
@@ -943,16 +965,30 @@ bool run_score_comb(int dtype, const ScoreCombArgs& a, const ScoreArgs& sa, hipS
 }
 
 // Microseconds per 128-byte slice, as in fwd_tile_of of vpce_kernels.hip.
-FwdTile score_tile_f8(int kind) {
-  using G0 = GemmF8<false>;
-  if (kind == 0) return FwdTile{G0::BM, G0::BN, G0::OCC, 1.4, 1.8};
-  return FwdTile{RingF8::BM, RingF8::BN, RingF8::OCC, 0.47, 0.5};
+FwdTile score_tile(int dtype, int kind) {
+  using M = ScoreCfg<F32>::Middle;
+  if (dtype == VP_F32 && kind == 1) return FwdTile{M::BM, M::BN, M::OCC, 3.95, 3.95};
+  if (dtype != VP_E4M3) return fwd_tile(dtype, kind);
+  using L = ScoreCfg<F8>::Large;
+  using S = ScoreCfg<F8>::Small;
+  if (kind == 0) return FwdTile{L::BM, L::BN, L::OCC, 1.4, 1.8};
+  return FwdTile{S::BM, S::BN, S::OCC, 0.47, 0.5};
 }
 
-int score_coarse(int kind) {
-  using C = Cfg<Bf16>;
-  static_assert(RingF8::WGM == C::Stream64::WGM && GemmF8<false>::WGM == C::Logits::WGM, "the types' tiles are alike");
-  return 2 * (kind == 0 ? C::Logits::WGM : kind == 1 ? C::Stream128::WGM : C::Stream64::WGM);
+// f of the tile that a problem runs on
+template <class F>
+static int of_tile(int dtype, int kind, F&& f) {
+  using B = ScoreCfg<Bf16>;
+  using C = ScoreCfg<F8>;
+  using D = ScoreCfg<F32>;
+  static_assert(B::Large::WGM == C::Large::WGM && B::Large::WGM == D::Large::WGM && B::Small::WGM == C::Small::WGM &&
+                    B::Small::WGM == D::Small::WGM,
+                "the types' tiles are alike");
+  if (kind == 1) return dtype == VP_F32 ? f(D::Middle{}) : f(B::Middle{});
+  return kind == 0 ? f(B::Large{}) : f(B::Small{});
+}
+int score_coarse(int dtype, int kind) {
+  return of_tile(dtype, kind, [](auto g) { return 2 * decltype(g)::WGM; });
 }
 
 // Up to 512 tokens, two workgroups of 1024 a CU, the latency of a token counts.
@@ -965,12 +1001,8 @@ static bool launch_top(const TopArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((top_kernel<E, 256>), grid, dim3(256), 0, s, a);
   return launched_ok();
 }
-int score_tokens(int kind) {
-  using C = Cfg<Bf16>;
-  static_assert(kFineTokens<GemmF8<false>> == kFineTokens<C::Logits> && kFineTokens<RingF8> == kFineTokens<C::Stream64> &&
-                    kFineTokens<C::Stream128> == kFineTokens<C::Stream64>,
-                "by the kind of tile alone");
-  return kind == 0 ? kFineTokens<C::Logits> : kFineTokens<C::Stream64>;
+int score_tokens(int dtype, int kind) {
+  return of_tile(dtype, kind, [](auto g) { return kFineTokens<decltype(g)>; });
 }
 
 bool run_top(int dtype, const TopArgs& a, hipStream_t s) {
