@@ -205,6 +205,11 @@ StripPlan strip_plan(const vp_problem* p) {
   return s;
 }
 
+// What of it strips and partial sums of dH may take.
+int64_t strips_and_sums(const vp_problem* p, const StripPlan& s) {
+  return (int64_t)s.total - (int64_t)kHeaderBytes - (int64_t)align256((size_t)p->T * 4) - 5 * 256;
+}
+
 size_t bwd_ws_bytes(const vp_problem* p) { return strip_plan(p).total; }
 
 void build_table(const vp_problem* p, const void* const* W_shards, int bm, vpce::ShardTable* st,
@@ -257,6 +262,7 @@ struct BwdStrip {  // vocabulary side of the strips; each meets every token chun
 };
 struct BwdPlan {
   int cls = 0, slots = 1;
+  int least_jobs = 1;  // dH jobs of a strip with enough slices for them
   int64_t Tc = 0, Vc = 0;  // Vc: most padded rows a strip may have
   double time = -1;
   // filled in by cut_strips
@@ -361,15 +367,16 @@ double plan_time(const vp_problem* p, const BwdPlan& f) {
 // longer chunks would make less exact: H of mean 8 and deviation 1, T = 10^6, d = 64, V = 64,
 // dW off float64 by 1.8e-6 in chains of 10240 tokens and by 6.5e-6 in chains of 500032.
 //
-// many_jobs (a loss with an entropy term): of plans that differ in dH partial sums alone and are
-// estimated alike, float32 takes the one with room for the most: fewer of them may not go into the
-// shards' boundaries and leave long jobs (T = 1333, d = 1000, V = 32003 in 5: two jobs 2.54 ms, three
-// 2.29; T = 300, d = 2048, V = 50000 in 4: 1.85 and 1.72; bfloat16 within 3% either way).
-BwdPlan plan_bwd(const vp_problem* p, bool many_jobs = false) {
+// short_jobs (a loss with an entropy term): in float32 a strip's dH sum is cut into six jobs at least
+// where the workspace holds them.  Two tiles run on a CU side by side and a strip without a next one
+// has no residual tiles in its launch, so one or two jobs may be longer than all the rest (us, before and
+// now: T = 1333, d = 1000, V = 32003 in 5 2303 / 2120; T = 4000 6775 / 6645; T = 3300, d = 1280, V = 3413 871 /
+// 817; 22 random problems 0.94 to 1.01 of it, and with more jobs up to 1.05; bfloat16 within 3%).
+BwdPlan plan_bwd(const vp_problem* p, bool short_jobs = false) {
   const StripPlan s = strip_plan(p);
   const int64_t eb = (int64_t)elem_bytes(p->dtype);
   const int64_t budget = p->strip_elems > 0 ? p->strip_elems : kDefaultStrip;
-  const int64_t avail = (int64_t)s.total - (int64_t)kHeaderBytes - (int64_t)align256((size_t)p->T * 4) - 5 * 256;
+  const int64_t avail = strips_and_sums(p, s);
   const int64_t slot = p->T * p->d * 4;
   BwdPlan best;
   auto consider = [&](int cls, int slots, int64_t Tc, int64_t Vc) {
@@ -379,8 +386,7 @@ BwdPlan plan_bwd(const vp_problem* p, bool many_jobs = false) {
     f.Tc = Tc;
     f.Vc = Vc;
     f.time = plan_time(p, f);
-    const bool more = many_jobs && p->dtype == VP_F32 && cls == best.cls && Tc == best.Tc && f.time == best.time;
-    if (best.time < 0 || f.time < best.time || more) best = std::move(f);
+    if (best.time < 0 || f.time < best.time) best = std::move(f);
   };
   consider(3, 1, s.Tc, s.Vc);
   for (int cls = p->dtype == VP_BF16 ? 0 : 1; cls < 3; ++cls) {
@@ -402,6 +408,7 @@ BwdPlan plan_bwd(const vp_problem* p, bool many_jobs = false) {
       }
     }
   }
+  if (short_jobs && p->dtype == VP_F32 && best.cls != 3) best.least_jobs = 6;
   return best;
 }
 
@@ -418,13 +425,19 @@ void cut_strips(const vp_problem* p, BwdPlan* f) {
   const int64_t N = std::min(f->Tc, p->T), n_tb = ceil_div(N, ft.bn);
   const int64_t n_nb = vpce::bwd_col_blocks(f->cls, (int)p->d);
   bool used[vpce::kMaxJobs] = {false};
+  for (const BwdStrip& st : f->strips) f->Vr = std::max(f->Vr, st.rows_pad);
+  if (f->least_jobs > 1) {
+    const int64_t room = strips_and_sums(p, strip_plan(p)) - 4 * f->Tc * f->Vr * eb;
+    f->slots = (int)std::max<int64_t>(f->slots, std::min<int64_t>(vpce::kMaxJobs, room / (p->T * p->d * 4)));
+  }
   for (BwdStrip& st : f->strips) {
-    f->Vr = std::max(f->Vr, st.rows_pad);
     int64_t ks = 0;
     for (const BwdStrip::Seg& sg : st.segs) ks += ceil_div(sg.rows, KB);
     const int64_t work = st.rows_pad / ft.bm * n_tb * ceil_div(p->d, KB) +
                          ceil_div(st.rows_pad, ft.bn) * n_nb * ceil_div(N, KB) + n_tb * n_nb * ks;
     int64_t per = job_slices(ks, work, f->slots);
+    if (f->least_jobs > 1)
+      per = std::max(std::min(per, std::max<int64_t>(8, ceil_div(ks, f->least_jobs))), ceil_div(ks, f->slots));
     auto add = [&](int seg, int n_seg, int64_t k0, int64_t rows) {
       const size_t j = st.jobs.size();
       st.jobs.push_back({seg, n_seg, (int32_t)k0, (int32_t)rows, used[j] ? 1 : 0});
