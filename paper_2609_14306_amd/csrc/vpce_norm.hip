@@ -15,6 +15,9 @@
 // MI355X, kernels alone, averages: T = 32768, d = 2880, bfloat16 forward 74 us (5.1 TB/s; 69.2
 // among others of its kind), backward 172 + 4.8 us (5.5 TB/s); T = 16384, d = 7168, float32
 // without a mean 165 us (5.7 TB/s) and 263 + 4.8 us (5.4 TB/s); a 1 GiB copy runs at 5.1 TB/s.
+// With a residual (X + R stored and normalised; dS added in the backward), bfloat16 without a mean:
+// T = 32768, d = 2880 with the result in 8 bits 120 us (7 bytes an element, 5.5 TB/s), backward T = 16384,
+// d = 7168 301 + 5 us (14 bytes, 5.5 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
