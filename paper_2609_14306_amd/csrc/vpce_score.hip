@@ -25,11 +25,10 @@
 // at half the rate.
 //
 // What bounds it (kernels alone).  Many tokens: the matrix rate at the clock that the chip's power
-// leaves: T = 4096, d = 2880, V = 201088 in bfloat16 3.69 ms (1284 TFLOP/s, as vp_ce_forward; 3.88 and 0.22
+// leaves: T = 4096, d = 2880, V = 201088 in bfloat16 3.69 ms (1284 TFLOP/s, as vp_ce_forward; 3.88 and 0.20
 // for the ranking with 8 alternatives), T = 8192, d = 7168, V = 129280 in 8 bits 5.46 ms (2780), T = 1000, d =
 // 7168, V = 32000 in float32 3.36 ms (137).  Few tokens: reading W: T = 1, d = 4096, V = 151936 in bfloat16
-// 228 us (5.5 TB/s) and 38 for 20 alternatives, T = 40 in 8 bits 131 us (4.8 TB/s; 116, 5.4, at best) and
-// 20 for 5.
+// 218 us (5.7 TB/s) and 30 for 20 alternatives, T = 40 in 8 bits 121 us (5.2 TB/s) and 18 for 5.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -656,7 +655,10 @@ __global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreA
 // The most likely ids of a token, one workgroup of NT threads each, which finishes the token too.
 // Bound by latency for few tokens (a few dependent reads of maxima, then four rows of W for each group
 // of ids that is looked at; 16 wavefronts side by side), and for many by those rows: (K + 2) 4 d
-// elements a token.
+// elements a token.  Of the 30 us of T = 1, d = 4096, K = 20 in bfloat16 3 are the threshold, 2 the groups, 13 the
+// rows in two turns, most of it their conversion to float64 (units of two rows, which convert h twice, took
+// 6 more), and 3 the order.  Comparisons of all with all go a lane each, counted by ballots: one thread
+// for each of 88 logits took 5 us longer.
 constexpr int kExtra = 2, kMaxGroups = VP_MAX_TOP + kExtra;
 constexpr int kCoarseRoom = 512, kFineRoom = 1024;
 constexpr int kKeep = 4;  // fours of coarse maxima that a thread keeps in registers
@@ -773,12 +775,15 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
   int n = count[1];
   if (fits) {
     groups = min(n, want);
-    for (int e = tid; e < n; e += NT) {
+    for (int e = wave; e < n; e += WAVES) {  // (a lane compares with every 64th other one)
       const float v = cand_v[e];
       const int g = cand_g[e];
       int r = 0;
-      for (int k = 0; k < n; ++k) r += before(cand_v[k], cand_g[k], v, g);
-      if (r < want) sel[r] = g;
+      for (int k = 0; k < n; k += 64) {
+        const int o = min(k + lane, n - 1);
+        r += __popcll(__ballot(k + lane < n && before(cand_v[o], cand_g[o], v, g)));
+      }
+      if (r < want && lane == 0) sel[r] = g;
     }
     for (int base = 0; tied && groups < want && base < f.n_tiles * F; base += NT) {
       const int g = base + tid;
@@ -850,7 +855,7 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
     const int row = (tile - f.st.tile0[pos]) * a.bm + g % F * 4, live = min(4, f.st.rows[pos] - row);
     const uint4* w = (const uint4*)((const S*)f.st.w[pos] + (int64_t)row * f.d);
     double acc[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll 2
+#pragma unroll (NT == 1024 ? 4 : 2)
     for (int c = lane; c < chunks; c += 64) {
       double x[N], y[N];
       uint4 raw[4];
@@ -871,14 +876,18 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
         acc[r] = fma(p, scale, acc[r]);
       }
     }
+    // the four sums over the lanes: two of them to each half of the wavefront, then one to each quarter
+    const bool up = lane & 32, odd = lane & 16;
+    double two[2];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
+    for (int r = 0; r < 2; ++r) two[r] = (up ? acc[2 + r] : acc[r]) + __shfl_xor(up ? acc[r] : acc[2 + r], 32);
+    double v = (odd ? two[1] : two[0]) + __shfl_xor(odd ? two[0] : two[1], 16);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc[r] += __shfl_xor(acc[r], o);
-    if (lane < 4) {
-      const double v = lane == 0 ? acc[0] : lane == 1 ? acc[1] : lane == 2 ? acc[2] : acc[3];
-      val[4 * s + lane] = v;
-      gid[4 * s + lane] = lane < live ? f.st.off[pos] + row + lane : -1;
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if ((lane & 15) == 0) {
+      const int r = lane >> 4;
+      val[4 * s + r] = v;
+      gid[4 * s + r] = r < live ? f.st.off[pos] + row + r : -1;
     }
   }
   __syncthreads();
@@ -891,24 +900,26 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
     return;
   }
   n = 4 * groups;
-  if (tid < n && gid[tid] >= 0) {
-    const double v = val[tid];
-    const int64_t g = gid[tid];
+  int live = 0;
+  for (int k = 0; k < n; k += 64) live += __popcll(__ballot(k + lane < n && gid[min(k + lane, n - 1)] >= 0));
+  for (int e = wave; e < n; e += WAVES) {
+    const double v = val[e];
+    const int64_t g = gid[e];
+    if (g < 0) continue;
     int r = 0;
-    for (int k = 0; k < n; ++k) r += gid[k] >= 0 && before(val[k], gid[k], v, g);
-    if (r < a.top) {
+    for (int k = 0; k < n; k += 64) {
+      const int o = min(k + lane, n - 1);
+      r += __popcll(__ballot(k + lane < n && gid[o] >= 0 && before(val[o], gid[o], v, g)));
+    }
+    if (r < a.top && lane == 0) {
       ids[r] = g;
       loss[r] = (float)((double)lse - v);
     }
   }
   // fewer ids than asked for
-  if (tid == 0) {
-    int live = 0;
-    for (int k = 0; k < n; ++k) live += gid[k] >= 0;
-    for (int k = live; k < a.top; ++k) {
-      ids[k] = -1;
-      loss[k] = INFINITY;
-    }
+  if (tid >= live && tid < a.top) {
+    ids[tid] = -1;
+    loss[tid] = INFINITY;
   }
 }
 
