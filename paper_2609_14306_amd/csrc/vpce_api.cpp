@@ -129,7 +129,8 @@ int64_t count_tiles(const vp_problem* p, int bm) {
 struct FwdPlan {
   int kind, splits;
 };
-FwdPlan plan_fwd(const vp_problem* p, int64_t slots, vpce::FwdTile (*tile)(int, int) = vpce::fwd_tile) {
+FwdPlan plan_fwd(const vp_problem* p, int64_t slots, vpce::FwdTile (*tile)(int, int) = vpce::fwd_tile,
+                 int kinds = vpce::kFwdKinds) {
   FwdPlan best{0, splits_for(p)};
   if (p->T > kFewTokens) {
     // Whole tiles on the 256 x 256 tile again: where splits_for's workgroups leave a last
@@ -156,9 +157,9 @@ FwdPlan plan_fwd(const vp_problem* p, int64_t slots, vpce::FwdTile (*tile)(int, 
     return best;
   }
   double best_time = 0;
-  for (int kind = 0; kind < vpce::kFwdKinds; ++kind) {
-    if (kind == 1 && p->dtype == VP_E4M3) continue;  // (not built)
+  for (int kind = 0; kind < kinds; ++kind) {
     const vpce::FwdTile t = tile(p->dtype, kind);
+    if (t.per_cu == 0) continue;
     const int64_t blocks = ceil_div(p->T, t.bn), places = kCUs * t.per_cu;
     const int64_t tiles = std::max<int64_t>(1, count_tiles(p, t.bm));
     int64_t S = std::max<int64_t>(1, std::min(std::min(slots / p->T, places / blocks), tiles));
@@ -1005,7 +1006,7 @@ vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, con
   char* base = (char*)ws;
   for (int64_t t0 = 0; t0 < prob->T; t0 += plan.Tc) {
     const int64_t T = part.T = std::min(plan.Tc, prob->T - t0);
-    const FwdPlan fp = plan_fwd(&part, plan.slots, vpce::score_tile);
+    const FwdPlan fp = plan_fwd(&part, plan.slots, vpce::score_tile, vpce::kScoreKinds);
     const vpce::FwdTile ft = vpce::score_tile(prob->dtype, fp.kind);
     vpce::TopArgs a;
     memset(&a, 0, sizeof(a));

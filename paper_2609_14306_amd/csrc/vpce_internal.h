@@ -47,6 +47,7 @@ struct CombArgs {
 // Tiles the forward can run on: kind 0 is the 256 x 256 tile of every large problem,
 // the others are the streamed tiles for few tokens.
 constexpr int kFwdKinds = 3;
+constexpr int kScoreKinds = 4;  // of the scoring kernels (score_tile): 3 is for float32 alone
 struct FwdTile {
   int bm, bn;             // vocabulary rows by tokens
   int per_cu;             // workgroups a CU holds
@@ -237,7 +238,7 @@ bool run_fwd(int dtype, const FwdArgs& a, hipStream_t s);
 bool run_comb(const CombArgs& a, hipStream_t s);
 int score_coarse(int dtype, int kind);  // coarse maxima of a tile
 int score_tokens(int dtype, int kind);  // tokens side by side in the fine maxima
-FwdTile score_tile(int dtype, int kind);  // fwd_tile of the scoring kernels
+FwdTile score_tile(int dtype, int kind);  // fwd_tile of the scoring kernels; per_cu 0: not built
 bool run_score(int dtype, const ScoreArgs& a, hipStream_t s);
 bool run_score_comb(int dtype, const ScoreCombArgs& a, const ScoreArgs& sa, hipStream_t s);
 bool run_top(int dtype, const TopArgs& a, hipStream_t s);

@@ -942,10 +942,13 @@ static bool launch_score_stream(const ScoreArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((score_stream_kernel<E, G, false>), grid, dim3(G::NT), 0, s, a);
   return launched_ok();
 }
-// The tiles of the forward, but for float32's middle one: the 128 x 128 tile of its backward, of
-// which two workgroups share a CU, reaches 136 TFLOP/s against the streamed one's 121 and the large
-// one's 144 (d = 2880, V = 50000, microseconds: T = 128 386 -> 375, T = 384 1163 -> 1073, T = 1024
-// 2629 -> 2492; d = 1000, V = 32003: T = 1333 806 -> 792, T = 1536 976 -> 905).
+// The tiles of the forward, but for float32, whose products are bound by their matrix rate down to 20
+// tokens.  There two workgroups share a CU on all but the large tile: middle, the 128 x 128 tile of the
+// backward; small, 128 x 64 with a ring of three slices; least, 128 x 32.  They reach 136, 134 and 107
+// TFLOP/s (the large one 144) and leave shorter last rounds; the forward's tiles, of which one fits on a CU,
+// reach 121 (256 x 128) and 101 (128 x 64).  d = 2880, V = 50000 in 4, microseconds with the forward's and with
+// these: T = 1 248 / 139, T = 64 252 / 205, T = 128 386 / 373, T = 384 1163 / 912, T = 1024 2629 / 2344, T =
+// 2048 4588 / 4440; d = 1000, V = 32003 in 5: T = 1333 806 / 760.
 template <class E> struct ScoreCfg {
   using Large = typename Cfg<E>::Logits;
   using Small = typename Cfg<E>::Stream64;
@@ -958,8 +961,9 @@ template <> struct ScoreCfg<F8> {
 };
 template <> struct ScoreCfg<F32> {
   using Large = Cfg<F32>::Logits;
-  using Small = Cfg<F32>::Stream64;
+  using Small = Cfg<F32>::Res128x64;
   using Middle = Cfg<F32>::Res128;
+  using Least = Ring<128, 32, 4, 1, 3, F32>;
 };
 template <class E>
 static bool launch_score(const ScoreArgs& a, hipStream_t s) {
@@ -967,8 +971,10 @@ static bool launch_score(const ScoreArgs& a, hipStream_t s) {
   if (a.f.kind == 2) return launch_score_stream<E, typename C::Small>(a, s);
   if constexpr (sizeof(typename E::storage) == 2)
     if (a.f.kind == 1) return launch_score_stream<E, typename C::Middle>(a, s);
-  if constexpr (sizeof(typename E::storage) == 4)
+  if constexpr (sizeof(typename E::storage) == 4) {
     if (a.f.kind == 1) return launch_score_g<E, typename C::Middle>(a, s);
+    if (a.f.kind == 3) return launch_score_stream<E, typename C::Least>(a, s);
+  }
   if (a.f.d % E::KB == 0) return launch_score_g<E, typename C::Large>(a, s);
   return launch_score_g<E, typename Cfg<E>::LogitsTail>(a, s);
 }
@@ -990,13 +996,18 @@ bool run_score_comb(int dtype, const ScoreCombArgs& a, const ScoreArgs& sa, hipS
 
 // Microseconds per 128-byte slice, as in fwd_tile_of of vpce_kernels.hip.
 FwdTile score_tile(int dtype, int kind) {
-  using M = ScoreCfg<F32>::Middle;
-  if (dtype == VP_F32 && kind == 1) return FwdTile{M::BM, M::BN, M::OCC, 3.95, 3.95};
+  if (dtype == VP_F32 && kind > 0) {
+    using C = ScoreCfg<F32>;
+    if (kind == 1) return FwdTile{C::Middle::BM, C::Middle::BN, C::Middle::OCC, 3.95, 3.95};
+    if (kind == 2) return FwdTile{C::Small::BM, C::Small::BN, C::Small::OCC, 2.0, 2.2};
+    return FwdTile{C::Least::BM, C::Least::BN, C::Least::OCC, 1.25, 1.5};
+  }
+  if (kind == 3) return FwdTile{0, 0, 0, 0.0, 0.0};
   if (dtype != VP_E4M3) return fwd_tile(dtype, kind);
-  using L = ScoreCfg<F8>::Large;
-  using S = ScoreCfg<F8>::Small;
-  if (kind == 0) return FwdTile{L::BM, L::BN, L::OCC, 1.4, 1.8};
-  return FwdTile{S::BM, S::BN, S::OCC, 0.47, 0.5};
+  using C = ScoreCfg<F8>;
+  if (kind == 0) return FwdTile{C::Large::BM, C::Large::BN, C::Large::OCC, 1.4, 1.8};
+  if (kind == 1) return FwdTile{0, 0, 0, 0.0, 0.0};
+  return FwdTile{C::Small::BM, C::Small::BN, C::Small::OCC, 0.47, 0.5};
 }
 
 // f of the tile that a problem runs on
@@ -1008,6 +1019,7 @@ static int of_tile(int dtype, int kind, F&& f) {
   static_assert(B::Large::WGM == C::Large::WGM && B::Large::WGM == D::Large::WGM && B::Small::WGM == C::Small::WGM &&
                     B::Small::WGM == D::Small::WGM,
                 "the types' tiles are alike");
+  if (kind == 3) return f(D::Least{});
   if (kind == 1) return dtype == VP_F32 ? f(D::Middle{}) : f(B::Middle{});
   return kind == 0 ? f(B::Large{}) : f(B::Small{});
 }

@@ -102,7 +102,7 @@ int main(int argc, char** argv) {
   auto log_int = [&](double lo, double hi) {
     return (int64_t)exp(std::uniform_real_distribution<double>(log(lo), log(hi))(r));
   };
-  int kinds[3][vpce::kFwdKinds] = {{0}}, chunks = 0;
+  int kinds[3][vpce::kScoreKinds] = {{0}}, chunks = 0;
   for (int n = 0; n < 1500; ++n) {
     vp_problem p;
     memset(&p, 0, sizeof(p));
@@ -127,9 +127,9 @@ int main(int argc, char** argv) {
   }
   bool all = chunks > 0;
   for (int t = 0; t < 3; ++t)
-    for (int k = 0; k < vpce::kFwdKinds; ++k) {
+    for (int k = 0; k < vpce::kScoreKinds; ++k) {
       printf("%d ", kinds[t][k]);
-      all = all && (kinds[t][k] > 0 || (t == VP_E4M3 && k == 1));
+      all = all && (kinds[t][k] > 0) == (vpce::score_tile(t, k).per_cu > 0);
     }
   printf("launches by type and kind; %d in chunks\n", chunks);
   return all ? 0 : 1;

@@ -70,8 +70,10 @@ def test_every_tile(kind, dtype, T, d, rows):
 SIZES = [("bf16", 1, 8, [1]), ("bf16", 1, 4096, [3001]), ("f32", 1, 72, [5, 0, 4]), ("bf16", 3, 64, [255, 256, 257]),
          ("f32", 64, 520, [1000]), ("bf16", 65, 200, [33] * 11), ("f32", 2300, 200, [1000, 513]),
          ("bf16", 2300, 64, [1000, 0, 2001]), ("bf16", 2600, 1000, [1333, 4003]), ("bf16", 300, 16, [4, 3, 2, 1]),
-         # float32's 128 x 128 tile
-         ("f32", 700, 200, [5000, 3001, 9]), ("f32", 100, 72, [20001, 5, 30000]), ("f32", 1100, 40, [12000, 5001])]
+         # float32's tiles: 128 x 128, 128 x 64 and 128 x 32
+         ("f32", 700, 200, [5000, 3001, 9]), ("f32", 100, 72, [20001, 5, 30000]), ("f32", 1100, 40, [12000, 5001]),
+         ("f32", 1030, 72, [5000, 3001, 9]), ("f32", 64, 1000, [60000, 300]), ("f32", 20, 1000, [3001, 0, 129]),
+         ("f32", 33, 104, [20001, 127]), ("f32", 32, 2880, [128, 70001])]
 
 
 @pytest.mark.parametrize("top", [1, 5, 32])
