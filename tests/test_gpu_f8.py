@@ -88,7 +88,9 @@ def check_f8(H, Hs, W, Ws, t, got, top, ignore=-100):
 @pytest.mark.parametrize("T, d, rows", [
     (1, 16, [1]), (1, 4096, [3001]), (3, 128, [127, 129, 0, 256]), (40, 2880, [700, 4097]), (64, 112, [300]),
     (65, 272, [1000]), (300, 640, [255, 3000]), (2100, 256, [1000, 513]), (2300, 400, [2001]), (2600, 1040, [1333, 4003]),
-    (2049, 128, [256]), (2500, 384, [300, 5, 128, 129, 640])])
+    (2049, 128, [256]), (2500, 384, [300, 5, 128, 129, 640]),
+    # the tile of 128 tokens
+    (100, 14336, [3001, 0, 500]), (128, 272, [40000]), (90, 1040, [20001, 127, 30000]), (127, 144, [60000])])
 def test_score_of_8_bit_operands(T, d, rows, top):
     ops = make(T, d, rows, seed=top)
     check_f8(*ops, vp.score_f8(*ops, top=top), top)
