@@ -1,9 +1,10 @@
 """8-bit operands on the GPU: quantisation value for value against the plain form, and scoring of
 such operands against float64 of the values that they stand for.
 
-The matrix unit's sums of 8-bit products are rounded more coarsely than float32 ones; a logit is held
-to the same worst-case bound as there, (d + 2) u sum |h w|, which is far above what either does.
-loss and top_loss have float64 logits, so only lse's error, an average over the vocabulary, enters."""
+The matrix unit cuts eight products at a time off at 2^-13 of the largest one's power of two, i.e. each of
+the seven others by less than 2^-13 of the largest: no more than 7 2^-13 of the eight magnitudes' sum. So a
+logit is held to (7 2^-13 + (d + 2) u) sum |h w| (float32 sums alone, (d + 2) u, hold it only where many
+products or ids average that out).  loss and top_loss have float64 logits, so only lse's error enters."""
 import pytest
 import torch
 
@@ -81,7 +82,21 @@ def make(T, d, rows, seed=0, spread=2.0):
 
 
 def check_f8(H, Hs, W, Ws, t, got, top, ignore=-100):
-    check(sp.values(H, Hs, 1), [sp.values(w, s, 128) for w, s in zip(W, Ws)], t, got, top, ignore)
+    check(sp.values(H, Hs, 1), [sp.values(w, s, 128) for w, s in zip(W, Ws)], t, got, top, ignore,
+          product=7 * 2.0 ** -13)
+
+
+@pytest.mark.parametrize("T", [300, 2100])
+@pytest.mark.parametrize("d", [16, 64, 112, 512, 4096])
+def test_rounding_of_a_single_sum(T, d):
+    """With one id lse is its logit: the sum of the products as the matrix unit rounds it, 1.5e-5 of the sums'
+    root mean square (held to twice that), on the small tiles and the large one."""
+    H, Hs, W, Ws, t = make(T, d, [1], spread=0.0)
+    lse = vp.score_f8(H, Hs, W, Ws, t)[1].double()
+    h, w = sp.values(H, Hs, 1), sp.values(W[0], Ws[0], 128)
+    y = (h @ w.t().contiguous())[:, 0]
+    assert bool(((lse - y).abs() <= (7 * 2.0 ** -13 + (d + 2) * sp.U) * (h.abs() @ w.abs().t().contiguous())[:, 0]).all())
+    assert float((lse - y).square().mean().sqrt()) <= 3e-5 * float((h.square() @ w.square().t().contiguous()).mean().sqrt())
 
 
 @pytest.mark.parametrize("top", [0, 1, 20])

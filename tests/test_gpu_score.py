@@ -29,8 +29,9 @@ def make(dtype, T, d, rows, seed=0, scale=2.0):
     return H, W, t
 
 
-def check(H, W, t, got, top, ignore=-100, exact_ids=True):
-    """got: (loss, lse, entropy, ids, top_loss) against float64, 512 tokens at a time."""
+def check(H, W, t, got, top, ignore=-100, exact_ids=True, product=0.0):
+    """got: (loss, lse, entropy, ids, top_loss) against float64, 512 tokens at a time.  product: what the
+    products lose before they are summed, of sum_k |h_k w_k|."""
     loss, lse, entropy, ids, top_loss = got
     W64 = torch.cat(W).double()
     V = W64.shape[0]
@@ -38,7 +39,8 @@ def check(H, W, t, got, top, ignore=-100, exact_ids=True):
         s = slice(a, a + 512)
         H64 = H[s].double()
         want = sp.score(H64, W64, t[s], ignore, top)
-        b = sp.logit_bound(H64, W64) + sp.fold_bound(V) + 2 * U * want[1].abs()
+        e_y = sp.logit_bound(H64, W64) * (1 + product / ((H64.shape[1] + 2) * U))
+        b = e_y + sp.fold_bound(V) + 2 * U * want[1].abs()
 
         def within(x, y, bound, what):
             assert torch.equal(x.isnan(), y.isnan()), what
@@ -49,7 +51,7 @@ def check(H, W, t, got, top, ignore=-100, exact_ids=True):
         within(lse[s], want[1], b, "lse")
         within(loss[s], want[0], b + U * want[0].abs(), "loss")
         S = want[2]
-        within(entropy[s], S, 2 * sp.logit_bound(H64, W64) * (S + 1) + (2 * sp.fold_bound(V) + 8 * U) * (S + 1) + 8 * U,
+        within(entropy[s], S, 2 * e_y * (S + 1) + (2 * sp.fold_bound(V) + 8 * U) * (S + 1) + 8 * U,
                "entropy")
         assert bool((loss[s][t[s] == ignore] == 0).all())
         if top:
