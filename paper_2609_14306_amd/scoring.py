@@ -14,7 +14,7 @@ from functools import cached_property
 
 from . import (VP_E4M3, VP_ERR_WORKSPACE, Problem, _check, _dtype_code, _need, _need_ws, _same_device, _torch_dtype,
                load_library, problem_for, vp_ce_workspace_size, vp_quant, vp_score)
-from .head import _bytes, _call, _f32, _raw_stream, _spec
+from .head import _bytes, _call, _f32, _raw_stream, _spec, layer_norm
 
 
 class Score:
@@ -197,9 +197,16 @@ def _score_outputs(T: int, score: Score, like):
     return [_f32(T, like=like) for _ in range(3)] + (list(top) if score.top else [None, None])
 
 
-def score(H, W_shards, targets, top: int = 0, ignore_index: int = -100, ws=None):
+def score(H, W_shards, targets, top: int = 0, ignore_index: int = -100, ws=None, norm=None):
     """(loss, lse, entropy, top_ids, top_loss) of hidden states H [T, d] and shards W_p [V_p, d]; the
-    last two [T, top], or None without alternatives."""
+    last two [T, top], or None without alternatives.
+
+    With `norm` (a ``HeadNorm``, as ``forward`` and ``backward`` take it), H is what the norm takes."""
+    import torch
+    if norm is not None:
+        with torch.cuda.device_of(H):  # the norm and the projection on one stream
+            Y = layer_norm(H, norm.gamma, norm.beta, norm.eps, norm.rms)[0]
+            return score(Y, W_shards, targets, top, ignore_index, ws)
     prob, sc = problem_for(H, W_shards, ignore_index), Score(top)
     ws = _bytes(vp_score_workspace_size(prob, sc), H) if ws is None else ws
     out = _score_outputs(prob.T, sc, H)

@@ -131,7 +131,9 @@ def test_with_a_norm_in_front():
     _, W, t = make("f32", 200, 64, [300, 50])
     Y = vp.layer_norm(X, gamma, None, norm.eps, True)[0]
     g, e = upstream(200)
-    loss, lse, ent, _, _ = vp.score(Y, W, t)
+    loss, lse, ent, ids, top_loss = vp.score(Y, W, t, top=3)
+    for a, b in zip(vp.score(X, W, t, top=3, norm=norm), (loss, lse, ent, ids, top_loss)):
+        assert torch.equal(a, b)
     dX, dW, dgamma, _ = vp.backward(X, W, t, lse, g, norm=norm, entropy=ent, grad_entropy=e)
     x, ga = X.double().requires_grad_(), gamma.double().requires_grad_()
     y = x * ((x * x).mean(1, keepdim=True) + norm.eps).rsqrt() * ga
