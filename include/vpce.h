@@ -231,8 +231,8 @@ vp_status vp_ce_check(const void* ws, void* stream, int64_t* bad_targets);
  * infinity among the logits, or none above minus infinity), entropy and top_loss are NaN and
  * the ids -1.
  * The order is that of the exact logits: those of all candidates are taken again in float64.
- * (Candidates come from float32 logits, some more than asked for: three groups of four
- * consecutive ids within a rounding of each other at the last place can hide one.) */
+ * (Candidates come from the product's logits, some more than asked for, and up to 64 groups of four
+ * consecutive ids where they lie within the roundings of its sums: more that near can hide one.) */
 #define VP_MAX_TOP 32
 typedef struct {
   int32_t top; /* alternatives of every token, 0..VP_MAX_TOP (VP_ERR_VALUE otherwise) */

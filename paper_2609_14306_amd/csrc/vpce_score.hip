@@ -9,10 +9,11 @@
 //
 // Alternatives.  No logits are kept; the fold leaves the maximum of every four consecutive ids
 // (fine) and of the logits that a lane holds of a tile (coarse).  The K + 2 largest fine maxima,
-// ties by the lower ids, hold the K largest logits but for what float32 sums round: the logits of
+// ties by the lower ids, hold the K largest logits but for what the product's sums round: the logits of
 // those ids are taken again in float64, where the products of the operands are exact, and ranked by
-// that.  An answer differs from the float64 one only where three groups of ids lie within the
-// rounding of the sums at its border.
+// that.  Where the maxima come nearer to the last one given than eight times what the ones looked at are
+// off by, all that do are looked at, up to 64: an answer differs from the float64 one only where more
+// lie that near (1 to 2 us of a call).
 //
 // 8-bit operands (e4m3) have a power of two as scale for every 128 columns of a token and every 128
 // x 128 block of a shard.  A slice of 128 bytes is one such block: the matrix instruction of
@@ -665,7 +666,8 @@ __global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreA
 // rows in two turns, most of it their conversion to float64 (units of two rows, which convert h twice, took
 // 6 more), and 3 the order.  Comparisons of all with all go a lane each, counted by ballots: one thread
 // for each of 88 logits took 5 us longer.
-constexpr int kExtra = 2, kMaxGroups = VP_MAX_TOP + kExtra;
+constexpr int kExtra = 2, kGroupRoom = 64;
+static_assert(VP_MAX_TOP + kExtra <= kGroupRoom, "groups of a token");
 constexpr int kCoarseRoom = 512, kFineRoom = 1024;
 constexpr int kKeep = 4;  // fours of coarse maxima that a thread keeps in registers
 
@@ -682,9 +684,11 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
   __shared__ float side[WAVES][64];
   __shared__ float cand_v[kFineRoom];
   __shared__ int cand_g[kFineRoom], list[kCoarseRoom];
-  __shared__ int sel[kMaxGroups];
-  __shared__ double val[4 * kMaxGroups];
-  __shared__ int64_t gid[4 * kMaxGroups];
+  __shared__ int sel[kGroupRoom];
+  __shared__ float sel_v[kGroupRoom];
+  __shared__ double val[4 * kGroupRoom], last_s;
+  __shared__ int64_t gid[4 * kGroupRoom];
+  __shared__ unsigned off_s;
   __shared__ int count[2];
   __shared__ float tau_s, lse_s;
   __shared__ float best_v[WAVES];
@@ -789,7 +793,10 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
         const int o = min(k + lane, n - 1);
         r += __popcll(__ballot(k + lane < n && before(cand_v[o], cand_g[o], v, g)));
       }
-      if (r < want && lane == 0) sel[r] = g;
+      if (r < want && lane == 0) {
+        sel[r] = g;
+        sel_v[r] = v;
+      }
     }
     for (int base = 0; tied && groups < want && base < f.n_tiles * F; base += NT) {
       const int g = base + tid;
@@ -802,7 +809,10 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
         at += w < wave ? best_g[w] : 0;
         groups += best_g[w];
       }
-      if (hit >> lane & 1 && at < want) sel[at] = g;
+      if (hit >> lane & 1 && at < want) {
+        sel[at] = g;
+        sel_v[at] = tau;
+      }
       __syncthreads();
     }
     groups = min(groups, want);
@@ -843,89 +853,142 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
         }
       __syncthreads();
       if (g == INT32_MAX) break;
-      if (tid == 0) sel[groups] = g;
+      if (tid == 0) {
+        sel[groups] = g;
+        sel_v[groups] = v;
+      }
       last_v = v;
       last_g = g;
     }
   }
-  __syncthreads();
-  const uint4* h = (const uint4*)((const S*)f.H + t * f.d);
   const int chunks = f.d / N;
+  if (tid == 0) {
+    off_s = 0;
+    last_s = -INFINITY;
+  }
+  __syncthreads();
   if (wave == 0) {
     const float lse = finish_token<E>(a.comb, a.s, t, lane);
     if (lane == 0) lse_s = lse;
   }
-  for (int s = wave - 1; s < groups && wave > 0; s += WAVES - 1) {
-    const int g = __builtin_amdgcn_readfirstlane(sel[s]), tile = g / F;
-    const int pos = __popcll(__ballot(f.st.tile0[lane + 1] <= tile));  // (a shard a lane)
-    const int row = (tile - f.st.tile0[pos]) * a.bm + g % F * 4, live = min(4, f.st.rows[pos] - row);
-    const uint4* w = (const uint4*)((const S*)f.st.w[pos] + (int64_t)row * f.d);
-    double acc[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll (NT == 1024 ? 4 : 2)
-    for (int c = lane; c < chunks; c += 64) {
-      double x[N], y[N];
-      uint4 raw[4];
+  for (bool again = false;; again = true) {
+    for (int s = wave - 1; s < groups && wave > 0; s += WAVES - 1) {
+      const int g = __builtin_amdgcn_readfirstlane(sel[s]), tile = g / F;
+      const int pos = __popcll(__ballot(f.st.tile0[lane + 1] <= tile));  // (a shard a lane)
+      const int row = (tile - f.st.tile0[pos]) * a.bm + g % F * 4, live = min(4, f.st.rows[pos] - row);
+      const uint4* w = (const uint4*)((const S*)f.st.w[pos] + (int64_t)row * f.d);
+      // (H's row goes through an empty statement: the compiler would hold it for all groups in registers)
+      const uint4* h = (const uint4*)((const S*)f.H + t * f.d);
+      asm volatile("" : "+s"(h));
+      double acc[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll (NT != 1024 ? 2 : kIsF8<E> ? 1 : 4)  // (a lane of 1024 has 128 registers)
+      for (int c = lane; c < chunks; c += 64) {
+        double x[N], y[N];
+        uint4 raw[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) raw[r] = w[(int64_t)min(r, live - 1) * chunks + c];
-      Dot<E>::unpack(h[c], x);
-      double scale = 1.0;
-      if constexpr (kIsF8<E>) {
-        const int b = c / (128 / N);
-        scale = pow2_byte(a.s.h_scale[t * a.s.nb + b]) * pow2_byte(a.s.w_scale[pos][(int64_t)(row / 128) * a.s.nb + b]);
+        for (int r = 0; r < 4; ++r) raw[r] = w[(int64_t)min(r, live - 1) * chunks + c];
+        Dot<E>::unpack(h[c], x);
+        double scale = 1.0;
+        if constexpr (kIsF8<E>) {
+          const int b = c / (128 / N);
+          scale = pow2_byte(a.s.h_scale[t * a.s.nb + b]) * pow2_byte(a.s.w_scale[pos][(int64_t)(row / 128) * a.s.nb + b]);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          Dot<E>::unpack(raw[r], y);
+          double p = 0.0;
+#pragma unroll
+          for (int k = 0; k < N; ++k) p = fma(x[k], y[k], p);
+          acc[r] = fma(p, scale, acc[r]);
+        }
       }
+      // the four sums over the lanes: two of them to each half of the wavefront, then one to each quarter
+      const bool up = lane & 32, odd = lane & 16;
+      double two[2];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        Dot<E>::unpack(raw[r], y);
-        double p = 0.0;
+      for (int r = 0; r < 2; ++r) two[r] = (up ? acc[2 + r] : acc[r]) + __shfl_xor(up ? acc[r] : acc[2 + r], 32);
+      double v = (odd ? two[1] : two[0]) + __shfl_xor(odd ? two[0] : two[1], 16);
 #pragma unroll
-        for (int k = 0; k < N; ++k) p = fma(x[k], y[k], p);
-        acc[r] = fma(p, scale, acc[r]);
-      }
-    }
-    // the four sums over the lanes: two of them to each half of the wavefront, then one to each quarter
-    const bool up = lane & 32, odd = lane & 16;
-    double two[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r) two[r] = (up ? acc[2 + r] : acc[r]) + __shfl_xor(up ? acc[r] : acc[2 + r], 32);
-    double v = (odd ? two[1] : two[0]) + __shfl_xor(odd ? two[0] : two[1], 16);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    if ((lane & 15) == 0) {
+      for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o);
       const int r = lane >> 4;
-      val[4 * s + r] = v;
-      gid[4 * s + r] = r < live ? f.st.off[pos] + row + r : -1;
+      if ((lane & 15) == 0) {
+        val[4 * s + r] = v;
+        gid[4 * s + r] = r < live ? f.st.off[pos] + row + r : -1;
+      }
+      // what the float32 maximum is off by
+      double most = r < live ? v : -INFINITY;
+      most = fmax(most, __shfl_xor(most, 16));
+      most = fmax(most, __shfl_xor(most, 32));
+      const float off = (float)__builtin_fabs(most - (double)sel_v[s]);
+      if (lane == 0 && off < INFINITY) atomicMax(&off_s, __float_as_uint(off));
     }
-  }
-  __syncthreads();
-  const float lse = lse_s;
-  if (!(__builtin_fabsf(lse) < INFINITY)) {
-    if (tid < a.top) {
+    __syncthreads();
+    const float lse = lse_s;
+    if (!(__builtin_fabsf(lse) < INFINITY)) {
+      if (tid < a.top) {
+        ids[tid] = -1;
+        loss[tid] = __builtin_nanf("");
+      }
+      return;
+    }
+    n = 4 * groups;
+    int live = 0;
+    for (int k = 0; k < n; k += 64) live += __popcll(__ballot(k + lane < n && gid[min(k + lane, n - 1)] >= 0));
+    for (int e = wave; e < n; e += WAVES) {
+      const double v = val[e];
+      const int64_t g = gid[e];
+      if (g < 0) continue;
+      int r = 0;
+      for (int k = 0; k < n; k += 64) {
+        const int o = min(k + lane, n - 1);
+        r += __popcll(__ballot(k + lane < n && gid[o] >= 0 && before(val[o], gid[o], v, g)));
+      }
+      if (r < a.top && lane == 0) {
+        ids[r] = g;
+        loss[r] = (float)((double)lse - v);
+        if (r == a.top - 1) last_s = v;
+      }
+    }
+    // fewer ids than asked for
+    if (tid >= live && tid < a.top) {
       ids[tid] = -1;
-      loss[tid] = __builtin_nanf("");
+      loss[tid] = INFINITY;
     }
-    return;
-  }
-  n = 4 * groups;
-  int live = 0;
-  for (int k = 0; k < n; k += 64) live += __popcll(__ballot(k + lane < n && gid[min(k + lane, n - 1)] >= 0));
-  for (int e = wave; e < n; e += WAVES) {
-    const double v = val[e];
-    const int64_t g = gid[e];
-    if (g < 0) continue;
-    int r = 0;
-    for (int k = 0; k < n; k += 64) {
-      const int o = min(k + lane, n - 1);
-      r += __popcll(__ballot(k + lane < n && gid[o] >= 0 && before(val[o], gid[o], v, g)));
+    if (again || groups < want) return;
+    // A group that is not among them has a float32 maximum of sel_v[want - 1] at most, and one id of it a
+    // logit that is larger by what the sums are off by, for which eight times the most that was seen stands.
+    // Where that reaches the last logit that is given, all groups that could are looked at, if there is room.
+    __syncthreads();
+    const double last = last_s, margin = 8.0 * (double)__uint_as_float(off_s);
+    if ((double)sel_v[want - 1] + margin <= last || !(last > -INFINITY)) return;
+    __syncthreads();
+    if (tid == 0) count[1] = 0;
+    __syncthreads();
+    const float border = (float)(last - margin);
+#pragma unroll 1
+    for (int c = tid; c < n4; c += NT) {
+      const float4 v = coarse(c);
+#pragma unroll 1
+      for (int e = 0; e < 4 * fpc && max4(v) >= border; ++e) {
+        const int within = (4 * c + e / fpc) % cpt;
+        const int g = (4 * c + e / fpc) / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
+        const float x = fine(g);
+        const int k = x >= border ? atomicAdd(&count[1], 1) : kGroupRoom;
+        if (k < kGroupRoom) {
+          cand_v[k] = x;
+          cand_g[k] = g;
+        }
+      }
     }
-    if (r < a.top && lane == 0) {
-      ids[r] = g;
-      loss[r] = (float)((double)lse - v);
+    __syncthreads();
+    n = count[1];
+    if (n > kGroupRoom || n <= groups) return;
+    groups = n;
+    if (tid < n) {
+      sel[tid] = cand_g[tid];
+      sel_v[tid] = cand_v[tid];
     }
-  }
-  // fewer ids than asked for
-  if (tid >= live && tid < a.top) {
-    ids[tid] = -1;
-    loss[tid] = INFINITY;
+    __syncthreads();
   }
 }
 

@@ -141,6 +141,29 @@ def test_large_logits_in_few_shares():
         check(H[:9], [w], t[:9], vp.score(H[:9], [w], t[:9], top=8), 8)
 
 
+@pytest.mark.parametrize("T", [1, 600, 2100])
+@pytest.mark.parametrize("top", [1, 4, 32])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_closer_than_float32_holds(dtype, top, T):
+    """Fifty ids with logits of 100 + k 2^-25, which no float32 sum tells apart, in scrambled order among
+    others below 20: exact logits decide."""
+    g = torch.Generator().manual_seed(top)
+    d, rows, n = 64, [3000, 5000], 50
+    H = torch.randn(T, d, generator=g).cuda()
+    H[:, 0], H[:, 1] = 1.0, 2.0 ** -12
+    W = torch.randn(sum(rows), d, generator=g).cuda() / d ** 0.5
+    W[:, :2] = 0
+    at = (torch.randperm(sum(rows) // 8, generator=g)[:n] * 8 + 3).cuda()  # groups of their own
+    W[at] = 0
+    W[at, 0] = 100.0
+    W[at, 1] = torch.arange(n, device="cuda") * 2.0 ** -13
+    H, W = H.to(DT[dtype]), W.to(DT[dtype])
+    t = torch.zeros(T, dtype=torch.int64, device="cuda")
+    out = vp.score(H, list(W.split(rows)), t, top=top)
+    assert torch.equal(out[3], at.flip(0)[:top].expand(T, top))
+    check(H, list(W.split(rows)), t, out, top)
+
+
 def test_repeated_rows():
     """The same row under several ids, in several shards: the lower id first."""
     H, W, t = make("bf16", 300, 256, [600, 700, 800])
