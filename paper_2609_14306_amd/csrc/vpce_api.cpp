@@ -928,9 +928,11 @@ vp_status vp_score_backward(const vp_problem* prob, const void* H, const void* c
 
 namespace {
 
-// Scoring.  Without alternatives it is one forward over all tokens.  With them the maxima of the
-// logits (1 to 1.25 bytes for each logit, see vpce::ScoreArgs) wait in the workspace for the tokens'
-// workgroups, so the tokens go through in chunks whose maxima take at most kTopBytes, or of 256.
+// Scoring.  Without alternatives it is one forward over all tokens.  With them, and for 8-bit operands
+// (whose likely ids are looked up, see top_kernel), the maxima of the logits (1 to 1.25 bytes for each
+// logit, see vpce::ScoreArgs) wait in the workspace for the tokens' workgroups, so the tokens go through
+// in chunks whose maxima take at most kTopBytes (twice that where no alternatives are asked for: T = 8192,
+// V = 129280 in one chunk 3% faster than in two), or of 256.
 constexpr int64_t kTopBytes = 1ll << 30;
 constexpr int64_t kMaxTopV = 1ll << 24;
 
@@ -944,8 +946,9 @@ ScorePlan score_plan(const vp_problem* p, int top) {
   int64_t rows = 0;  // of the largest tiles, padding among them
   for (int q = 0; q < p->P; ++q) rows += round_up(p->shard_rows[q], 256);
   s.Tc = p->T;
-  if (top > 0) {
-    const int64_t most = std::max<int64_t>(256, round_down(kTopBytes / (rows + rows / 4), 256));
+  const bool maxima = top > 0 || p->dtype == VP_E4M3;
+  if (maxima) {
+    const int64_t most = std::max<int64_t>(256, round_down(kTopBytes * (top > 0 ? 1 : 2) / (rows + rows / 4), 256));
     if (p->T > most) s.Tc = round_up(ceil_div(p->T, ceil_div(p->T, most)), 256);
   }
   // Partial states for as many splits as the few tokens' tiles can take: partial_slots goes by the
@@ -961,8 +964,8 @@ ScorePlan score_plan(const vp_problem* p, int top) {
   s.off_s = s.off_m + plane;
   s.off_u = s.off_s + plane;
   s.off_fine = s.off_u + plane;
-  s.off_coarse = s.off_fine + (top > 0 ? align256((size_t)(round_up(s.Tc, 32) * rows)) : 0);
-  s.total = s.off_coarse + (top > 0 ? align256((size_t)(s.Tc * (rows / 4))) : 0);
+  s.off_coarse = s.off_fine + (maxima ? align256((size_t)(round_up(s.Tc, 32) * rows)) : 0);
+  s.total = s.off_coarse + (maxima ? align256((size_t)(s.Tc * (rows / 4))) : 0);
   return s;
 }
 
@@ -971,7 +974,7 @@ vp_status validate(const vp_problem* p, const vp_score* score, bool f8, int64_t*
   if (st != VP_OK) return st;
   if (!score) return VP_ERR_NULL;
   if (score->top < 0 || score->top > VP_MAX_TOP) return VP_ERR_VALUE;
-  if (score->top > 0 && *V > kMaxTopV) return VP_ERR_SHAPE;
+  if ((score->top > 0 || f8) && *V > kMaxTopV) return VP_ERR_SHAPE;
   return VP_OK;
 }
 
@@ -1023,7 +1026,7 @@ vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, con
     f.m_part = (float*)(base + plan.off_m);
     f.s_part = (float*)(base + plan.off_s);
     a.s.u_part = (float*)(base + plan.off_u);
-    if (top > 0) {
+    if (top > 0 || f8) {
       a.s.fine = (float*)(base + plan.off_fine);
       a.s.coarse = (float*)(base + plan.off_coarse);
     }
@@ -1047,7 +1050,7 @@ vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, con
     c.c.bad_counter = counter;
     c.u_part = a.s.u_part;
     c.entropy = entropy ? entropy + t0 : nullptr;
-    if (top == 0) {
+    if (top == 0 && !f8) {
       if (!vpce::run_score_comb(prob->dtype, c, a.s, s)) return VP_ERR_HIP;
       continue;
     }
@@ -1055,8 +1058,10 @@ vp_status score_impl(const vp_problem* prob, const vp_score* score, bool f8, con
     a.cpt = vpce::score_coarse(prob->dtype, fp.kind);
     a.tok = vpce::score_tokens(prob->dtype, fp.kind);
     a.top = top;
-    a.ids = top_ids + t0 * top;
-    a.loss = top_loss + t0 * top;
+    if (top > 0) {
+      a.ids = top_ids + t0 * top;
+      a.loss = top_loss + t0 * top;
+    }
     if (!vpce::run_top(prob->dtype, a, s)) return VP_ERR_HIP;
   }
   return VP_OK;

@@ -19,11 +19,13 @@
 // x 128 block of a shard.  A slice of 128 bytes is one such block: the matrix instruction of
 // 64 columns takes the scales as its own operands, for nothing.  It adds eight products of a row
 // with bits below 2^-13 of the largest one's power of two cut off, and such sums in float32 (as
-// measured; the instruction without scales is the same): 1.5e-5 of the root mean square of a sum of
-// 4096 products.  lse averages that over the ids; entropies stand 2e-7 to 6e-6 from float64 (float32
-// products: 1e-7).  Widened to bfloat16, where the products are exact, few tokens took 164 us instead of
-// 132 (T = 1 to 64, V = 151936, d = 4096) and 310 instead of 181 (T = 128), and large tiles would run
-// at half the rate.
+// measured; the instruction without scales and the 16 x 16 ones are the same): a logit is off by 1.5e-5
+// of the logits' spread.  Over many ids that averages out; where a few hold the probability it does not
+// (logits of spread 4: entropies 1e-5 off).  So the ids with a probability of 2^-7 and more have their
+// exact logits put into lse and entropy behind the fold (top_kernel, kHeavy): 1e-7 to 8e-7 then.  That
+// takes the maxima also without alternatives (T = 8192, d = 7168, V = 129280 6% of the time).  Widened to
+// bfloat16, where the products are exact, few tokens took 164 us instead of 132 (T = 1 to 64, V = 151936,
+// d = 4096), with one wavefront a SIMD 137 (T to 32) and 183, and large tiles would run at half the rate.
 //
 // What bounds it (kernels alone).  Many tokens: the matrix rate at the clock that the chip's power
 // leaves: T = 4096, d = 2880, V = 201088 in bfloat16 3.69 ms (1284 TFLOP/s, as vp_ce_forward; 3.88 and 0.20
@@ -598,8 +600,13 @@ __device__ __forceinline__ double pow2_byte(int b) {  // 2^(b - 127), NaN for 25
 // coarsely than a float32 one (2e-5 of a logit, d = 4096), which lse averages over the vocabulary and
 // a single logit does not (loss off by 2.8e-6 relative with the tile's, 6e-8 so); and a wave of the
 // product's kernel keeps no targets in registers that it needs for operands.
+struct Finished {
+  float lse, entropy;
+  double y;  // the target's logit
+  int64_t target;
+};
 template <class E>
-__device__ __forceinline__ float finish_token(const ScoreCombArgs& a, const ScoreArgs& sa, int64_t t, int lane) {
+__device__ __forceinline__ Finished finish_token(const ScoreCombArgs& a, const ScoreArgs& sa, int64_t t, int lane) {
   using S = typename E::storage;
   constexpr int N = Dot<E>::N;
   const int64_t tg = a.c.targets[t];
@@ -636,26 +643,35 @@ __device__ __forceinline__ float finish_token(const ScoreCombArgs& a, const Scor
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) y += __shfl_xor(y, o);
   }
-  if (lane) return lse;
+  return Finished{lse, (log_s - f.u / f.s) * kLn2, y, tg};
+}
+
+// Its results, by one lane.
+__device__ __forceinline__ void store_token(const ScoreCombArgs& a, int64_t t, const Finished& f) {
   float loss;
-  if (tg == a.c.ignore_index) {
+  if (f.target == a.c.ignore_index) {
     loss = 0.f;
-  } else if (tg < 0 || tg >= a.c.V) {
+  } else if (f.target < 0 || f.target >= a.c.V) {
     loss = __builtin_nanf("");
-    atomicAdd(a.c.bad_counter, 1ull);
   } else {
-    loss = (float)((double)lse - y);
+    loss = (float)((double)f.lse - f.y);
   }
-  a.c.lse[t] = lse;
+  a.c.lse[t] = f.lse;
   a.c.loss[t] = loss;
-  if (a.entropy) a.entropy[t] = (log_s - f.u / f.s) * kLn2;
-  return lse;
+  if (a.entropy) a.entropy[t] = f.entropy;
+}
+__device__ __forceinline__ void count_target(const ScoreCombArgs& a, int64_t target) {
+  if (target != a.c.ignore_index && (target < 0 || target >= a.c.V)) atomicAdd(a.c.bad_counter, 1ull);
 }
 
 template <class E>
 __global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreArgs sa) {
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t < a.c.T) finish_token<E>(a, sa, t, threadIdx.x & 63);
+  if (t >= a.c.T) return;
+  const Finished f = finish_token<E>(a, sa, t, threadIdx.x & 63);
+  if (threadIdx.x & 63) return;
+  store_token(a, t, f);
+  count_target(a, f.target);
 }
 
 // ---------------------------------------------------------------------------
@@ -669,6 +685,10 @@ __global__ void __launch_bounds__(256) score_comb_kernel(ScoreCombArgs a, ScoreA
 constexpr int kExtra = 2, kGroupRoom = 64;
 static_assert(VP_MAX_TOP + kExtra <= kGroupRoom, "groups of a token");
 constexpr int kCoarseRoom = 512, kFineRoom = 1024;
+// 8-bit operands: the ids with a probability of 2^-7 and more have their part in lse and in the entropy
+// exactly.  A logit is off by 1.5e-5 of the logits' spread, which the rest of the ids averages out: with
+// random logits of spread 4 entropies are off by 8e-7 relative, and 1.2e-5 without.
+constexpr float kHeavy = -7.f * 0.6931471805599453f;
 constexpr int kKeep = 4;  // fours of coarse maxima that a thread keeps in registers
 
 // The larger logit first, the lower id among equals.
@@ -711,154 +731,158 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
   auto fine = [&](int g) { return fine_t[((int64_t)(g / F) * ((T + tok - 1) / tok) * F + g % F) * tok]; };
   auto max4 = [](float4 v) { return fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)); };
 
-  // tau: the want-th largest of 64 maxima over the threads' shares, which as many coarse maxima
-  // reach
-  const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-  float4 keep[kKeep];
-  float mine = -INFINITY;
+  // (without alternatives, of 8-bit operands, none are selected here)
+  const bool any = !kIsF8<E> || a.top > 0;
+  int groups = 0, n = 0;
+  if (any) {
+    // tau: the want-th largest of 64 maxima over the threads' shares, which as many coarse maxima
+    // reach
+    const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    float4 keep[kKeep];
+    float mine = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < kKeep; ++k) keep[k] = tid + k * NT < n4 ? coarse(tid + k * NT) : none;
+    for (int k = 0; k < kKeep; ++k) keep[k] = tid + k * NT < n4 ? coarse(tid + k * NT) : none;
 #pragma unroll
-  for (int k = 0; k < kKeep; ++k) mine = fmaxf(mine, max4(keep[k]));
+    for (int k = 0; k < kKeep; ++k) mine = fmaxf(mine, max4(keep[k]));
 #pragma unroll 8
-  for (int c = tid + kKeep * NT; c < n4; c += NT) mine = fmaxf(mine, max4(coarse(c)));
-  side[wave][lane] = mine;
-  if (tid < 2) count[tid] = 0;
-  __syncthreads();
-  if (wave == 0) {
-    float all = mine;
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) all = fmaxf(all, side[w][lane]);
-    int rank = 0;
-#pragma unroll
-    for (int k = 0; k < 64; ++k) rank += before(lane_read(all, k), k, all, lane);
-    if (rank == want - 1) tau_s = all;
-  }
-  __syncthreads();
-  const float tau = tau_s;
-  // The fine maxima that reach tau, or with `above` lie above it, among cand_*; whether they fit.
-  auto collect = [&](bool above) {
-    auto in = [&](float x) { return above ? x > tau : x >= tau; };
-    auto take = [&](int c, float4 v) {
-      const float x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (in(x[j])) {
-          const int k = atomicAdd(&count[0], 1);
-          if (k < kCoarseRoom) list[k] = 4 * c + j;
-        }
-    };
-    if (in(mine)) {
-#pragma unroll
-      for (int k = 0; k < kKeep; ++k)
-        if (tid + k * NT < n4) take(tid + k * NT, keep[k]);
-      for (int c = tid + kKeep * NT; c < n4; c += NT) take(c, coarse(c));
-    }
-    __syncthreads();
-    const int n_coarse = count[0];
-    if (n_coarse > kCoarseRoom) return false;
-    for (int e = tid; e < n_coarse * fpc; e += NT) {
-      const int c = list[e / fpc], within = c % cpt;
-      const int g = c / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
-      const float v = fine(g);
-      if (in(v)) {
-        const int k = atomicAdd(&count[1], 1);
-        if (k < kFineRoom) {
-          cand_v[k] = v;
-          cand_g[k] = g;
-        }
-      }
-    }
-    __syncthreads();
-    return count[1] <= kFineRoom;
-  };
-  int groups = 0;
-  bool fits = collect(false), tied = false;
-  if (!fits) {
-    // Many logits equal tau (a token of zeros has nothing else): those above it, and of the equal
-    // ones the first.
-    __syncthreads();
+    for (int c = tid + kKeep * NT; c < n4; c += NT) mine = fmaxf(mine, max4(coarse(c)));
+    side[wave][lane] = mine;
     if (tid < 2) count[tid] = 0;
     __syncthreads();
-    tied = fits = collect(true);
-  }
-  int n = count[1];
-  if (fits) {
-    groups = min(n, want);
-    for (int e = wave; e < n; e += WAVES) {  // (a lane compares with every 64th other one)
-      const float v = cand_v[e];
-      const int g = cand_g[e];
-      int r = 0;
-      for (int k = 0; k < n; k += 64) {
-        const int o = min(k + lane, n - 1);
-        r += __popcll(__ballot(k + lane < n && before(cand_v[o], cand_g[o], v, g)));
-      }
-      if (r < want && lane == 0) {
-        sel[r] = g;
-        sel_v[r] = v;
-      }
+    if (wave == 0) {
+      float all = mine;
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) all = fmaxf(all, side[w][lane]);
+      int rank = 0;
+#pragma unroll
+      for (int k = 0; k < 64; ++k) rank += before(lane_read(all, k), k, all, lane);
+      if (rank == want - 1) tau_s = all;
     }
-    for (int base = 0; tied && groups < want && base < f.n_tiles * F; base += NT) {
-      const int g = base + tid;
-      const uint64_t hit = __ballot(g < f.n_tiles * F && fine(min(g, f.n_tiles * F - 1)) == tau);
-      if (lane == 0) best_g[wave] = __popcll(hit);
-      __syncthreads();
-      int at = groups + __popcll(hit & ((1ull << lane) - 1));
+    __syncthreads();
+    const float tau = tau_s;
+    // The fine maxima that reach tau, or with `above` lie above it, among cand_*; whether they fit.
+    auto collect = [&](bool above) {
+      auto in = [&](float x) { return above ? x > tau : x >= tau; };
+      auto take = [&](int c, float4 v) {
+        const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        at += w < wave ? best_g[w] : 0;
-        groups += best_g[w];
-      }
-      if (hit >> lane & 1 && at < want) {
-        sel[at] = g;
-        sel_v[at] = tau;
+        for (int j = 0; j < 4; ++j)
+          if (in(x[j])) {
+            const int k = atomicAdd(&count[0], 1);
+            if (k < kCoarseRoom) list[k] = 4 * c + j;
+          }
+      };
+      if (in(mine)) {
+#pragma unroll
+        for (int k = 0; k < kKeep; ++k)
+          if (tid + k * NT < n4) take(tid + k * NT, keep[k]);
+        for (int c = tid + kKeep * NT; c < n4; c += NT) take(c, coarse(c));
       }
       __syncthreads();
+      const int n_coarse = count[0];
+      if (n_coarse > kCoarseRoom) return false;
+      for (int e = tid; e < n_coarse * fpc; e += NT) {
+        const int c = list[e / fpc], within = c % cpt;
+        const int g = c / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
+        const float v = fine(g);
+        if (in(v)) {
+          const int k = atomicAdd(&count[1], 1);
+          if (k < kFineRoom) {
+            cand_v[k] = v;
+            cand_g[k] = g;
+          }
+        }
+      }
+      __syncthreads();
+      return count[1] <= kFineRoom;
+    };
+    bool fits = collect(false), tied = false;
+    if (!fits) {
+      // Many logits equal tau (a token of zeros has nothing else): those above it, and of the equal
+      // ones the first.
+      __syncthreads();
+      if (tid < 2) count[tid] = 0;
+      __syncthreads();
+      tied = fits = collect(true);
     }
-    groups = min(groups, want);
-  } else {
-    // More above tau than there is room for (they lie in few threads' shares): the groups one by one,
-    // each the next in order after the one before.
-    float last_v = INFINITY;
-    int last_g = -1;
-    for (; groups < want; ++groups) {
-      float v = -INFINITY;
-      int g = INT32_MAX;
-      for (int k = tid; k < f.n_tiles * F; k += NT) {
-        const float x = fine(k);
-        if (x == x && before(last_v, last_g, x, k) && before(x, k, v, g)) {
-          v = x;
-          g = k;
+    n = count[1];
+    if (fits) {
+      groups = min(n, want);
+      for (int e = wave; e < n; e += WAVES) {  // (a lane compares with every 64th other one)
+        const float v = cand_v[e];
+        const int g = cand_g[e];
+        int r = 0;
+        for (int k = 0; k < n; k += 64) {
+          const int o = min(k + lane, n - 1);
+          r += __popcll(__ballot(k + lane < n && before(cand_v[o], cand_g[o], v, g)));
+        }
+        if (r < want && lane == 0) {
+          sel[r] = g;
+          sel_v[r] = v;
         }
       }
+      for (int base = 0; tied && groups < want && base < f.n_tiles * F; base += NT) {
+        const int g = base + tid;
+        const uint64_t hit = __ballot(g < f.n_tiles * F && fine(min(g, f.n_tiles * F - 1)) == tau);
+        if (lane == 0) best_g[wave] = __popcll(hit);
+        __syncthreads();
+        int at = groups + __popcll(hit & ((1ull << lane) - 1));
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        const float vo = __shfl_xor(v, o);
-        const int go = __shfl_xor(g, o);
-        if (before(vo, go, v, g)) {
-          v = vo;
-          g = go;
+        for (int w = 0; w < WAVES; ++w) {
+          at += w < wave ? best_g[w] : 0;
+          groups += best_g[w];
         }
+        if (hit >> lane & 1 && at < want) {
+          sel[at] = g;
+          sel_v[at] = tau;
+        }
+        __syncthreads();
       }
-      if (lane == 0) {
-        best_v[wave] = v;
-        best_g[wave] = g;
-      }
-      __syncthreads();
+      groups = min(groups, want);
+    } else {
+      // More above tau than there is room for (they lie in few threads' shares): the groups one by one,
+      // each the next in order after the one before.
+      float last_v = INFINITY;
+      int last_g = -1;
+      for (; groups < want; ++groups) {
+        float v = -INFINITY;
+        int g = INT32_MAX;
+        for (int k = tid; k < f.n_tiles * F; k += NT) {
+          const float x = fine(k);
+          if (x == x && before(last_v, last_g, x, k) && before(x, k, v, g)) {
+            v = x;
+            g = k;
+          }
+        }
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w)
-        if (before(best_v[w], best_g[w], v, g)) {
-          v = best_v[w];
-          g = best_g[w];
+        for (int o = 32; o > 0; o >>= 1) {
+          const float vo = __shfl_xor(v, o);
+          const int go = __shfl_xor(g, o);
+          if (before(vo, go, v, g)) {
+            v = vo;
+            g = go;
+          }
         }
-      __syncthreads();
-      if (g == INT32_MAX) break;
-      if (tid == 0) {
-        sel[groups] = g;
-        sel_v[groups] = v;
+        if (lane == 0) {
+          best_v[wave] = v;
+          best_g[wave] = g;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w)
+          if (before(best_v[w], best_g[w], v, g)) {
+            v = best_v[w];
+            g = best_g[w];
+          }
+        __syncthreads();
+        if (g == INT32_MAX) break;
+        if (tid == 0) {
+          sel[groups] = g;
+          sel_v[groups] = v;
+        }
+        last_v = v;
+        last_g = g;
       }
-      last_v = v;
-      last_g = g;
     }
   }
   const int chunks = f.d / N;
@@ -867,9 +891,14 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
     last_s = -INFINITY;
   }
   __syncthreads();
+  Finished token;
   if (wave == 0) {
-    const float lse = finish_token<E>(a.comb, a.s, t, lane);
-    if (lane == 0) lse_s = lse;
+    token = finish_token<E>(a.comb, a.s, t, lane);
+    if (lane == 0) {
+      lse_s = token.lse;
+      if (!kIsF8<E>) store_token(a.comb, t, token);
+      count_target(a.comb, token.target);
+    }
   }
   for (bool again = false;; again = true) {
     for (int s = wave - 1; s < groups && wave > 0; s += WAVES - 1) {
@@ -923,13 +952,68 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
       if (lane == 0 && off < INFINITY) atomicMax(&off_s, __float_as_uint(off));
     }
     __syncthreads();
-    const float lse = lse_s;
+    float lse = lse_s;
     if (!(__builtin_fabsf(lse) < INFINITY)) {
       if (tid < a.top) {
         ids[tid] = -1;
         loss[tid] = __builtin_nanf("");
       }
+      if (kIsF8<E> && tid == 0) store_token(a.comb, t, token);
       return;
+    }
+    const float heavy = lse + kHeavy;
+    if constexpr (kIsF8<E>) {
+      // With the matrix unit's m and the exact m + c of the largest id of a group, p = e^z, z = m - lse:
+      //   A = sum p (e^c - 1),  B = sum p ((e^c - 1) (z + c) + c),
+      //   lse' = lse + log(1 + A),  entropy' = (entropy - B) / (1 + A) + log(1 + A).
+      if (wave == 0) {
+        const float m = lane < groups ? sel_v[lane] : -INFINITY;
+        float z = 0.f, c = 0.f, p = 0.f;
+        if (m >= heavy) {
+          double most = -INFINITY;
+          for (int r = 0; r < 4; ++r) most = gid[4 * lane + r] >= 0 ? fmax(most, val[4 * lane + r]) : most;
+          z = m - lse;
+          c = (float)(most - (double)m);
+          p = expf(z);
+        }
+        float far = __builtin_fabsf(c), up = p > 0.f ? z + c : 0.f;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+          far = fmaxf(far, __shfl_xor(far, o));
+          up = fmaxf(up, __shfl_xor(up, o));
+        }
+        // (c far from 0, of operands with a few products above all others: the sums themselves, over e^up)
+        const bool small = far < 0.5f;
+        const float e = small ? expm1f(c) : expf(z + c - up);
+        float A = p * e, B = p * __builtin_fmaf(e, z + c, c), P = p, Q = p * z;
+        if (!small) {
+          A = p > 0.f ? e : 0.f;
+          B = p > 0.f ? e * (z + c) : 0.f;
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+          A += __shfl_xor(A, o);
+          B += __shfl_xor(B, o);
+          P += __shfl_xor(P, o);
+          Q += __shfl_xor(Q, o);
+        }
+        Finished exact = token;
+        if (small) {
+          const float l = log1pf(A);
+          exact.lse += l;
+          exact.entropy = (token.entropy - B) / (1.f + A) + l;
+        } else {
+          const float mass = 1.f - P > 1e-6f ? 1.f - P : 0.f, rest = expf(-up), all = mass * rest + A, l = up + logf(all);
+          exact.lse += l;
+          exact.entropy = fmaxf(l - ((mass > 0.f ? fminf(-token.entropy - Q, 0.f) * rest : 0.f) + B) / all, 0.f);
+        }
+        if (lane == 0) {
+          best_v[0] = exact.lse;
+          store_token(a.comb, t, exact);
+        }
+      }
+      __syncthreads();
+      lse = best_v[0];
     }
     n = 4 * groups;
     int live = 0;
@@ -954,30 +1038,44 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
       ids[tid] = -1;
       loss[tid] = INFINITY;
     }
-    if (again || groups < want) return;
+    if (again || (any && groups < want)) return;
     // A group that is not among them has a float32 maximum of sel_v[want - 1] at most, and one id of it a
     // logit that is larger by what the sums are off by, for which eight times the most that was seen stands.
-    // Where that reaches the last logit that is given, all groups that could are looked at, if there is room.
+    // Where that reaches the last logit that is given, all groups that could are looked at, if there is room;
+    // and so are those that the sums above should have.
     __syncthreads();
-    const double last = last_s, margin = 8.0 * (double)__uint_as_float(off_s);
-    if ((double)sel_v[want - 1] + margin <= last || !(last > -INFINITY)) return;
+    const float least = any ? sel_v[want - 1] : INFINITY;
+    float border = INFINITY;
+    if (a.top > 0) {
+      const double last = last_s, margin = 8.0 * (double)__uint_as_float(off_s);
+      if ((double)least + margin > last && last > -INFINITY) border = (float)(last - margin);
+    }
+    if (kIsF8<E> && least >= heavy) border = fminf(border, heavy);
+    if (border == INFINITY) return;
     __syncthreads();
-    if (tid == 0) count[1] = 0;
+    if (tid < 2) count[tid] = 0;
     __syncthreads();
-    const float border = (float)(last - margin);
 #pragma unroll 1
     for (int c = tid; c < n4; c += NT) {
       const float4 v = coarse(c);
 #pragma unroll 1
-      for (int e = 0; e < 4 * fpc && max4(v) >= border; ++e) {
-        const int within = (4 * c + e / fpc) % cpt;
-        const int g = (4 * c + e / fpc) / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
-        const float x = fine(g);
-        const int k = x >= border ? atomicAdd(&count[1], 1) : kGroupRoom;
-        if (k < kGroupRoom) {
-          cand_v[k] = x;
-          cand_g[k] = g;
-        }
+      for (int j = 0; j < 4 && max4(v) >= border; ++j) {
+        const int k = (j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w) >= border ? atomicAdd(&count[0], 1) : kCoarseRoom;
+        if (k < kCoarseRoom) list[k] = 4 * c + j;
+      }
+    }
+    __syncthreads();
+    const int n_coarse = count[0];
+    if (n_coarse > kCoarseRoom) return;
+#pragma unroll 1
+    for (int e = tid; e < n_coarse * fpc; e += NT) {
+      const int c = list[e / fpc], within = c % cpt;
+      const int g = c / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
+      const float v = fine(g);
+      const int k = v >= border ? atomicAdd(&count[1], 1) : kGroupRoom;
+      if (k < kGroupRoom) {
+        cand_v[k] = v;
+        cand_g[k] = g;
       }
     }
     __syncthreads();
@@ -996,18 +1094,18 @@ __global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
 template <class E, class G>
 static bool launch_score_g(const ScoreArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(a.f.n_tok_blocks * a.f.n_splits));
-  if (a.fine)
+  if (kIsF8<E> || a.fine)
     hipLaunchKernelGGL((score_kernel<E, G, true>), grid, dim3(G::NT), 0, s, a);
-  else
+  else if constexpr (!kIsF8<E>)
     hipLaunchKernelGGL((score_kernel<E, G, false>), grid, dim3(G::NT), 0, s, a);
   return launched_ok();
 }
 template <class E, class G>
 static bool launch_score_stream(const ScoreArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(a.f.n_tok_blocks * a.f.n_splits));
-  if (a.fine)
+  if (kIsF8<E> || a.fine)
     hipLaunchKernelGGL((score_stream_kernel<E, G, true>), grid, dim3(G::NT), 0, s, a);
-  else
+  else if constexpr (!kIsF8<E>)
     hipLaunchKernelGGL((score_stream_kernel<E, G, false>), grid, dim3(G::NT), 0, s, a);
   return launched_ok();
 }
@@ -1059,7 +1157,6 @@ static bool launch_comb(const ScoreCombArgs& a, const ScoreArgs& sa, hipStream_t
   return launched_ok();
 }
 bool run_score_comb(int dtype, const ScoreCombArgs& a, const ScoreArgs& sa, hipStream_t s) {
-  if (dtype == VP_E4M3) return launch_comb<F8>(a, sa, s);
   return dtype == VP_BF16 ? launch_comb<Bf16>(a, sa, s) : launch_comb<F32>(a, sa, s);
 }
 

@@ -49,7 +49,8 @@ static bool check_score(const vp_problem& p, int top) {
                                   ws, bytes, nullptr)
             : vp_score_forward(&p, &score, H, W.data(), targets, loss, lse, entropy, ids, top_loss, ws, bytes,
                                nullptr)) == VP_OK);
-  CHECK(!scored.empty() && tops.size() == (top ? scored.size() : 0) && joined_tokens.size() == (top ? 0 : scored.size()));
+  const bool maxima = top || f8;
+  CHECK(!scored.empty() && tops.size() == (maxima ? scored.size() : 0) && joined_tokens.size() == (maxima ? 0 : scored.size()));
   int64_t t0 = 0, V = 0;
   for (int q = 0; q < p.P; ++q) V += p.shard_rows[q];
   for (size_t k = 0; k < scored.size(); ++k) {
@@ -70,13 +71,13 @@ static bool check_score(const vp_problem& p, int top) {
                                                           {(const char*)f.m_part, f.n_splits * f.T * 4},
                                                           {(const char*)f.s_part, f.n_splits * f.T * 4},
                                                           {(const char*)a.u_part, f.n_splits * f.T * 4}};
-    const vpce::ScoreCombArgs& c = top ? tops[k].comb : joined_tokens[k];
+    const vpce::ScoreCombArgs& c = maxima ? tops[k].comb : joined_tokens[k];
     CHECK(c.c.m_part == f.m_part && c.c.s_part == f.s_part && c.u_part == a.u_part && c.c.n_splits == f.n_splits);
     CHECK(c.c.T == f.T && c.c.V == V && c.c.loss == loss + t0 && c.c.lse == lse + t0 && c.entropy == entropy + t0);
     CHECK(c.c.targets == f.targets && (char*)c.c.bad_counter == ws);
-    if (top) {
+    if (maxima) {
       const vpce::TopArgs& x = tops[k];
-      CHECK(x.bm == t.bm && (x.cpt == 4 || x.cpt == 8) && x.tok >= 1 && x.ids == ids + t0 * top && x.loss == top_loss + t0 * top);
+      CHECK(x.bm == t.bm && (x.cpt == 4 || x.cpt == 8) && x.tok >= 1 && x.ids == (top ? ids + t0 * top : nullptr) && x.loss == (top ? top_loss + t0 * top : nullptr));
       parts.push_back({(const char*)a.fine, tiles * round_up(f.T, x.tok) * t.bm});
       parts.push_back({(const char*)a.coarse, tiles * f.T * x.cpt * 4});
     } else {

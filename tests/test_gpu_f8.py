@@ -187,3 +187,36 @@ def test_graph():
         assert all(torch.equal(a, b) for a, b in zip(out, want))
         vp.score_f8(*make(33, 128, [500]), top=1)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("top", [0, 1, 8])
+@pytest.mark.parametrize("T, d, rows", [(1, 96, [527]), (7, 464, [9000, 772]), (90, 512, [3000]), (600, 128, [20000, 6264]),
+                                        (2200, 512, [6000])])
+def test_likely_ids_have_their_exact_logits(T, d, rows, top):
+    """Logits of spread 4, where few ids hold the probability.  What is left of the matrix unit's rounding are
+    the ids below 2^-7 and the ones that are not the largest of their four.  Their logits are off by e, 3e-5 of
+    the sums' root mean square at most (test_rounding_of_a_single_sum), independently: lse by e sqrt(sum p^2) and
+    the entropy by e sqrt(sum p^2 (log p + S)^2), as root mean squares over the tokens.  Held to four of these,
+    and float32 roundings: 4 u of lse, and 4 u of lse + 1 in the entropy, whose terms are log p."""
+    H, Hs, W, Ws, t = make(T, d, rows, seed=5, spread=0.0)
+    Hs.view(torch.uint8).add_(1)  # twice the make's 2
+    got = vp.score_f8(H, Hs, W, Ws, t, top=top)
+    h, w = sp.values(H, Hs, 1), torch.cat([sp.values(a, b, 128) for a, b in zip(W, Ws)])
+    want = sp.score(h, w, t, -100, top)
+    y, lse, S = want[5], want[1], want[2]
+    exact = torch.zeros_like(y, dtype=torch.bool)
+    at = 0
+    for r in rows:
+        four = torch.nn.functional.pad(y[:, at:at + r], (0, -r % 4), value=-torch.inf).view(T, -1, 4)
+        exact[:, at:at + r] = (four == four.amax(2, keepdim=True)).view(T, -1)[:, :r]
+        at += r
+    logp = y - lse[:, None]
+    p = torch.where(exact & (logp > -7 * 0.6931), 0.0, logp.exp())
+    e = 3e-5 * (h.square() @ w.square().t().contiguous()).mean(1).sqrt()
+    rms = lambda v: float(v.square().mean().sqrt())  # noqa: E731
+    left = 4 * rms(e * p.square().sum(1).sqrt())
+    assert rms(got[1].double() - lse) <= left + 4 * sp.U * rms(lse)
+    left = 4 * rms(e * (p * (logp + S[:, None])).square().sum(1).sqrt())
+    assert rms(got[2].double() - S) <= left + 4 * sp.U * rms(lse + 1)
+    if top:
+        assert torch.equal(got[3], want[3])
