@@ -29,7 +29,7 @@
 //
 // What bounds it (kernels alone).  Many tokens: the matrix rate at the clock that the chip's power
 // leaves: T = 4096, d = 2880, V = 201088 in bfloat16 3.69 ms (1284 TFLOP/s, as vp_ce_forward; 3.88 and 0.20
-// for the ranking with 8 alternatives), T = 8192, d = 7168, V = 129280 in 8 bits 5.46 ms (2780), T = 1000, d =
+// for the ranking with 8 alternatives), T = 8192, d = 7168, V = 129280 in 8 bits 5.71 ms (2660; 5.46 without maxima) and 0.19, T = 1000, d =
 // 7168, V = 32000 in float32 3.36 ms (137).  Few tokens: reading W: T = 1, d = 4096, V = 151936 in bfloat16
 // 218 us (5.7 TB/s) and 30 for 20 alternatives, T = 40 in 8 bits 121 us (5.2 TB/s) and 18 for 5.
 #include <hip/hip_runtime.h>
@@ -697,8 +697,10 @@ __device__ __forceinline__ bool before(V va, I ia, V vb, I ib) {
   return va > vb || (va == vb && ia < ib);
 }
 
+// (Many tokens in bfloat16: five wavefronts a SIMD, for which it is held to 102 registers, T = 4096 0.24 -> 0.22 ms;
+// 8 bits would spill.)
 template <class E, int NT>
-__global__ void __launch_bounds__(NT) top_kernel(TopArgs a) {
+__global__ void __launch_bounds__(NT, NT == 256 && sizeof(typename E::storage) == 2 ? 5 : 1) top_kernel(TopArgs a) {
   using S = typename E::storage;
   constexpr int N = Dot<E>::N, WAVES = NT / 64;
   __shared__ float side[WAVES][64];
