@@ -62,7 +62,8 @@ FwdTile fwd_tile(int dtype, int kind);
 // c % 2 of them for k < fpc = bm / 4 / cpt, counted from (c / 2) (2 fpc).
 struct ScoreArgs {
   FwdArgs f;
-  float* u_part;  // [n_splits][T]: sum of 2^x x, x the exponent (below 0) in s_part's sum
+  // (a part's state is m_part the maximum logit, s_part sum e^(y - m) - 1 and u_part sum e^(y - m) (y - m))
+  float* u_part;  // [n_splits][T]
   // [n_tiles][ceil(T / tok)][bm / 4][tok] with `tok` tokens side by side (score_tokens), NaN where no
   // row is live; null without alternatives
   float* fine;
