@@ -1089,9 +1089,16 @@ __global__ void __launch_bounds__(NT, NT == 256 && sizeof(typename E::storage) =
     n = count[1];
     if (n > kGroupRoom || n <= groups) return;
     groups = n;
-    if (tid < n) {
-      sel[tid] = cand_g[tid];
-      sel_v[tid] = cand_v[tid];
+    // (in their own order, not in the one that they came in: sums over them are the same bits every time)
+    const int own = min(lane, n - 1), g = cand_g[own];
+    const float v = cand_v[own];
+    for (int k = wave; k < n; k += WAVES) {
+      const float vk = lane_read(v, k);
+      const int gk = __builtin_amdgcn_readlane(g, k), r = __popcll(__ballot(lane < n && before(v, g, vk, gk)));
+      if (lane == 0) {
+        sel[r] = gk;
+        sel_v[r] = vk;
+      }
     }
     __syncthreads();
   }
