@@ -1052,42 +1052,47 @@ __global__ void __launch_bounds__(NT, NT == 256 && sizeof(typename E::storage) =
     // and so are those that the sums above should have.
     __syncthreads();
     const float least = any ? sel_v[want - 1] : INFINITY;
-    float border = INFINITY;
+    float near = INFINITY;
     if (a.top > 0) {
       const double last = last_s, margin = 8.0 * (double)__uint_as_float(off_s);
-      if ((double)least + margin > last && last > -INFINITY) border = (float)(last - margin);
+      if ((double)least + margin > last && last > -INFINITY) near = (float)(last - margin);
     }
-    if (kIsF8<E> && least >= heavy) border = fminf(border, heavy);
-    if (border == INFINITY) return;
-    __syncthreads();
-    if (tid < 2) count[tid] = 0;
-    __syncthreads();
+    const float likely = kIsF8<E> && least >= heavy ? heavy : INFINITY;
+    // (one of the two lists holds the other; where the longer one has no room the shorter one may)
+    float border = fminf(near, likely), other = fmaxf(near, likely);
+    for (;; border = other, other = INFINITY) {
+      if (border == INFINITY) return;
+      __syncthreads();
+      if (tid < 2) count[tid] = 0;
+      __syncthreads();
 #pragma unroll 1
-    for (int c = tid; c < n4; c += NT) {
-      const float4 v = coarse(c);
+      for (int c = tid; c < n4; c += NT) {
+        const float4 v = coarse(c);
 #pragma unroll 1
-      for (int j = 0; j < 4 && max4(v) >= border; ++j) {
-        const int k = (j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w) >= border ? atomicAdd(&count[0], 1) : kCoarseRoom;
-        if (k < kCoarseRoom) list[k] = 4 * c + j;
+        for (int j = 0; j < 4 && max4(v) >= border; ++j) {
+          const int k = (j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w) >= border ? atomicAdd(&count[0], 1) : kCoarseRoom;
+          if (k < kCoarseRoom) list[k] = 4 * c + j;
+        }
       }
-    }
-    __syncthreads();
-    const int n_coarse = count[0];
-    if (n_coarse > kCoarseRoom) return;
+      __syncthreads();
+      const int n_coarse = count[0];
+      if (n_coarse > kCoarseRoom) continue;
 #pragma unroll 1
-    for (int e = tid; e < n_coarse * fpc; e += NT) {
-      const int c = list[e / fpc], within = c % cpt;
-      const int g = c / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
-      const float v = fine(g);
-      const int k = v >= border ? atomicAdd(&count[1], 1) : kGroupRoom;
-      if (k < kGroupRoom) {
-        cand_v[k] = v;
-        cand_g[k] = g;
+      for (int e = tid; e < n_coarse * fpc; e += NT) {
+        const int c = list[e / fpc], within = c % cpt;
+        const int g = c / cpt * F + (within >> 1) * 2 * fpc + 2 * (e % fpc) + (within & 1);
+        const float v = fine(g);
+        const int k = v >= border ? atomicAdd(&count[1], 1) : kGroupRoom;
+        if (k < kGroupRoom) {
+          cand_v[k] = v;
+          cand_g[k] = g;
+        }
       }
+      __syncthreads();
+      n = count[1];
+      if (n <= kGroupRoom) break;
     }
-    __syncthreads();
-    n = count[1];
-    if (n > kGroupRoom || n <= groups) return;
+    if (n <= groups) return;
     groups = n;
     // (in their own order, not in the one that they came in: sums over them are the same bits every time)
     const int own = min(lane, n - 1), g = cand_g[own];

@@ -1,4 +1,6 @@
-"""8-bit scoring where the matrix unit's cut of small products shows: the same token has the same bits.
+"""8-bit scoring where the matrix unit's cut of small products shows: likely ids have their exact logits in lse and
+entropy whatever the alternatives need, alternatives are looked for whatever the likely ids need, and the same token
+has the same bits.
 
 ``built``: one token, as often as wanted.  A pair of products of +-P in one group of eight cuts the group's six others,
 which are below 2^-13 P: an id's product is 0 short by c = 1 to 6 of them, exactly (every number here is exact in 8
@@ -47,6 +49,28 @@ def held(got, want):
 
 
 T = [1, 30, 100, 600, 2100]
+
+
+@pytest.mark.parametrize("T", T)
+@pytest.mark.parametrize("big", [8.0, 32.0])
+@pytest.mark.parametrize("top", [0, 2])
+def test_likely_ids_beside_many_near_alternatives(top, big, T):
+    """An id of 0.30, thirty of 0.009 (above 2^-7) and sixty of 0.0071: with alternatives more ids than there is room
+    for lie near the second one, and the thirty alone have room."""
+    ops, want = built(T, [3.5] + [0.0] * 30 + [-0.25] * 60, [0] + [6] * 3 + [1 + k % 6 for k in range(27)] + [0] * 60, big)
+    got = vp.score_f8(*ops, top=top)
+    held(got, want)
+    if top:
+        assert torch.equal(got[3], want[3][:, :top].expand(T, top))
+
+
+@pytest.mark.parametrize("T", T)
+def test_near_alternatives_beside_many_likely_ids(T):
+    """Ninety-five ids above 2^-7, more than there is room for; the largest logit is the last of five that the
+    product does not tell apart."""
+    ops, want = built(T, [1.0] * 5 + [0.0] * 90, [1, 2, 3, 4, 5] + [0] * 90, 8.0)
+    got = vp.score_f8(*ops, top=1)
+    assert torch.equal(got[3], want[3][:, :1].expand(T, 1))
 
 
 @pytest.mark.parametrize("T", [30, 600, 2100])
