@@ -231,8 +231,10 @@ vp_status vp_ce_check(const void* ws, void* stream, int64_t* bad_targets);
  * infinity among the logits, or none above minus infinity), entropy and top_loss are NaN and
  * the ids -1.
  * The order is that of the exact logits: those of all candidates are taken again in float64.
- * (Candidates come from the product's logits, some more than asked for, and up to 64 groups of four
- * consecutive ids where they lie within the roundings of its sums: more that near can hide one.) */
+ * (Candidates are the groups of four consecutive ids with the `top` + 2 largest logits of the product, and
+ * where others come near the last answer, up to 64 groups.  Near is within eight times what the product's
+ * logits of the first ones are off by, and within 2.4e-7 sqrt(d) of the answer's size, or 6.1e-5 of it in 8 bits:
+ * an id whose sum is off by more than that, or more groups that near, can be missed.) */
 #define VP_MAX_TOP 32
 typedef struct {
   int32_t top; /* alternatives of every token, 0..VP_MAX_TOP (VP_ERR_VALUE otherwise) */

@@ -89,6 +89,7 @@ struct TopArgs {
   int32_t bm, cpt, tok, top;
   int64_t* ids;  // [T][top]
   float* loss;   // [T][top]
+  double sum_off;  // set by run_top: what a logit of the product may be off by, of itself
 };
 
 // Quantisation to 8 bits (vp_f8_quantize).

@@ -16,8 +16,8 @@
 // ties by the lower ids, hold the K largest logits but for what the product's sums round: the logits of
 // those ids are taken again in float64, where the products of the operands are exact, and ranked by
 // that.  Where the maxima come nearer to the last one given than eight times what the ones looked at are
-// off by, all that do are looked at, up to 64: an answer differs from the float64 one only where more
-// lie that near (1 to 2 us of a call).
+// off by, or than a rule for sums of d terms (run_top), all that do are looked at, up to 64: an answer differs from the
+// float64 one only where more lie that near, or a sum is off by more (1 to 2 us of a call).
 //
 // 8-bit operands (e4m3) have a power of two as scale for every 128 columns of a token and every 128
 // x 128 block of a shard.  A slice of 128 bytes is one such block: the matrix instruction of
@@ -38,6 +38,8 @@
 // 218 us (5.7 TB/s) and 30 for 20 alternatives, T = 40 in 8 bits 121 us (5.2 TB/s) and 18 for 5.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <cmath>
 
 #include "vpce_internal.h"
 #include "vpce_lanes.h"
@@ -560,6 +562,7 @@ struct Dot;
 template <>
 struct Dot<Bf16> {
   static constexpr int N = 8;
+  static constexpr uint32_t MAGNITUDE = 0x7fff7fffu;
   __device__ static void unpack(uint4 u, double (&f)[N]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -572,6 +575,7 @@ struct Dot<Bf16> {
 template <>
 struct Dot<F32> {
   static constexpr int N = 4;
+  static constexpr uint32_t MAGNITUDE = 0x7fffffffu;
   __device__ static void unpack(uint4 u, double (&f)[N]) {
     f[0] = (double)__uint_as_float(u.x);
     f[1] = (double)__uint_as_float(u.y);
@@ -582,6 +586,7 @@ struct Dot<F32> {
 template <>
 struct Dot<F8> {
   static constexpr int N = 16;
+  static constexpr uint32_t MAGNITUDE = 0x7f7f7f7fu;
   __device__ static void unpack(uint4 u, double (&f)[N]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
     typedef float f32x2_t __attribute__((ext_vector_type(2)));
@@ -1047,15 +1052,22 @@ __global__ void __launch_bounds__(NT, NT == 256 && sizeof(typename E::storage) =
     }
     if (again || (any && groups < want)) return;
     // A group that is not among them has a float32 maximum of sel_v[want - 1] at most, and one id of it a
-    // logit that is larger by what the sums are off by, for which eight times the most that was seen stands.
-    // Where that reaches the last logit that is given, all groups that could are looked at, if there is room;
-    // and so are those that the sums above should have.
+    // logit that is larger by what the sums are off by, for which eight times the most that was seen stands, and
+    // a.sum_off of the logit at least: the ones seen may be exact.  Where that reaches the last logit that is given,
+    // all groups that could are looked at, if there is room; and so are those that the sums above should have.
+    // (A token of zeros has exact logits, all equal.)
     __syncthreads();
     const float least = any ? sel_v[want - 1] : INFINITY;
     float near = INFINITY;
-    if (a.top > 0) {
-      const double last = last_s, margin = 8.0 * (double)__uint_as_float(off_s);
-      if ((double)least + margin > last && last > -INFINITY) near = (float)(last - margin);
+    const double last = last_s, margin = fmax(8.0 * (double)__uint_as_float(off_s), a.sum_off * __builtin_fabs(last));
+    if (a.top > 0 && (double)least + margin >= last && last > -INFINITY) {
+      uint32_t bits = 0;  // of H's row, but for signs
+#pragma unroll 1
+      for (int c = tid; c < chunks; c += NT) {
+        const uint4 h = ((const uint4*)((const S*)f.H + t * f.d))[c];
+        bits |= (h.x | h.y | h.z | h.w) & Dot<E>::MAGNITUDE;
+      }
+      if (__syncthreads_or((int)bits)) near = __double2float_rd(last - margin);
     }
     const float likely = kIsF8<E> && least >= heavy ? heavy : INFINITY;
     // (one of the two lists holds the other; where the longer one has no room the shorter one may)
@@ -1214,7 +1226,10 @@ int score_coarse(int dtype, int kind) {
 
 // Up to 512 tokens, two workgroups of 1024 a CU, the latency of a token counts.
 template <class E>
-static bool launch_top(const TopArgs& a, hipStream_t s) {
+static bool launch_top(TopArgs a, hipStream_t s) {
+  // A float32 sum of d products has as many roundings at most, of partial sums of about its size, which mostly
+  // cancel; the 8-bit products' cut is 1.5e-5.  Four times either.
+  a.sum_off = kIsF8<E> ? 0x1p-14 : 0x1p-22 * std::sqrt((double)a.s.f.d);
   const dim3 grid((unsigned)a.s.f.T);
   if (a.s.f.T <= 512)
     hipLaunchKernelGGL((top_kernel<E, 1024>), grid, dim3(1024), 0, s, a);
