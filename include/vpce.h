@@ -242,7 +242,7 @@ typedef struct {
 
 /* Workspace of vp_score_forward and vp_score_forward_f8 in bytes.  Host only.  With alternatives,
  * and for 8-bit operands always, it holds maxima of the logits of a chunk of tokens, at most 1 GiB
- * of them (2 GiB without alternatives) or those of 256 tokens, 1.25 bytes for each of a chunk's
+ * of them (2 GiB for 8-bit operands) or those of 256 tokens, 1.25 bytes for each of a chunk's
  * logits, and V is at most 2^24 (VP_ERR_SHAPE otherwise).  Otherwise it does not depend on V. */
 vp_status vp_score_workspace_size(const vp_problem* prob, const vp_score* score, size_t* bytes);
 

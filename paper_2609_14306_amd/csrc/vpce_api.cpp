@@ -931,9 +931,12 @@ namespace {
 // Scoring.  Without alternatives it is one forward over all tokens.  With them, and for 8-bit operands
 // (whose likely ids are looked up, see top_kernel), the maxima of the logits (1 to 1.25 bytes for each
 // logit, see vpce::ScoreArgs) wait in the workspace for the tokens' workgroups, so the tokens go through
-// in chunks whose maxima take at most kTopBytes (twice that where no alternatives are asked for: T = 8192,
-// V = 129280 in one chunk 3% faster than in two), or of 256.
-constexpr int64_t kTopBytes = 1ll << 30;
+// in chunks whose maxima take at most 1 GiB, or of 256.  8-bit operands have twice that: their products take half the
+// time, and a chunk's ends, where CUs wait for the last tiles, weigh twice (us, 1 and 2 GiB: T = 8192, d = 7168, V =
+// 129280 in 8 6042 / 5840, with an alternative 6255 / 6062; T = 6000, d = 4096, V = 151936 in 16 3309 / 3247, with 8
+// 3507 / 3450; T = 9001, d = 1024, V = 130001 in 2 1549 / 1488; T = 16000, d = 2048, V = 100000 in 4, 5 alternatives,
+// 3418 / 3405).
+constexpr int64_t top_bytes(int dtype) { return dtype == VP_E4M3 ? 2ll << 30 : 1ll << 30; }
 constexpr int64_t kMaxTopV = 1ll << 24;
 
 struct ScorePlan {
@@ -948,7 +951,7 @@ ScorePlan score_plan(const vp_problem* p, int top) {
   s.Tc = p->T;
   const bool maxima = top > 0 || p->dtype == VP_E4M3;
   if (maxima) {
-    const int64_t most = std::max<int64_t>(256, round_down(kTopBytes * (top > 0 ? 1 : 2) / (rows + rows / 4), 256));
+    const int64_t most = std::max<int64_t>(256, round_down(top_bytes(p->dtype) / (rows + rows / 4), 256));
     if (p->T > most) s.Tc = round_up(ceil_div(p->T, ceil_div(p->T, most)), 256);
   }
   // Partial states for as many splits as the few tokens' tiles can take: partial_slots goes by the
