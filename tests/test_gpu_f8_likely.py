@@ -1,6 +1,6 @@
 """8-bit scoring where the matrix unit's cut of small products shows: likely ids have their exact logits in lse and
-entropy whatever the alternatives need, alternatives are looked for whatever the likely ids need, and the same token
-has the same bits.
+entropy whatever the alternatives need, alternatives are looked for whatever the likely ids need, the same token has
+the same bits, and wide rows are held to root mean squares.
 
 ``built``: one token, as often as wanted.  A pair of products of +-P in one group of eight cuts the group's six others,
 which are below 2^-13 P: an id's product is 0 short by c = 1 to 6 of them, exactly (every number here is exact in 8
@@ -83,3 +83,27 @@ def test_equal_tokens_have_equal_bits(top, big, T):
     held(got, want)
     for x in got[:3] + (got[3:] if top else ()):
         one_value(x)
+
+
+@pytest.mark.parametrize("top", [0, 3])
+@pytest.mark.parametrize("d", [4096, 14336])
+@pytest.mark.parametrize("T, rows", [(40, [3001, 0, 700]), (128, [30000]), (2100, [1500, 601])])
+def test_wide_rows_with_scales_that_vary(T, rows, d, top):
+    """As test_gpu_f8.py's test_likely_ids_have_their_exact_logits, with the same 3e-5 of the sums' root mean square
+    for a logit, on wide rows whose scales differ from block to block."""
+    from test_gpu_f8 import make
+    H, Hs, W, Ws, t = make(T, d, rows, seed=3)
+    got = vp.score_f8(H, Hs, W, Ws, t, top=top)
+    h, w = sp.values(H, Hs, 1), torch.cat([sp.values(a, b, 128) for a, b in zip(W, Ws)])
+    want = sp.score(h, w, t, -100, top)
+    y, lse, S = want[5], want[1], want[2]
+    logp = y - lse[:, None]
+    p = logp.exp()
+    e = 3e-5 * (h.square() @ w.square().t().contiguous()).mean(1).sqrt()
+    rms = lambda v: float(v.square().mean().sqrt())  # noqa: E731
+    left = 4 * rms(e * p.square().sum(1).sqrt())
+    assert rms(got[1].double() - lse) <= left + 4 * U * rms(lse)
+    left = 4 * rms(e * (p * (logp + S[:, None])).square().sum(1).sqrt())
+    assert rms(got[2].double() - S) <= left + 4 * U * rms(lse + 1)
+    if top:
+        assert torch.equal(got[3], want[3])
