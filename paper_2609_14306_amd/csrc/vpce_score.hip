@@ -237,12 +237,6 @@ struct RingF8 : Ring<128, BN_, 4, 2, STAGES_, F8> {
   }
 };
 
-template <> struct Cfg<F8> {
-  using Logits = GemmF8<false>;
-  using LogitsTail = GemmF8<true>;
-  using Stream64 = RingF8<64, 6>;
-};
-
 // ---------------------------------------------------------------------------
 // A lane's state of a token: the maximum m, r = sum e^(y - m) - 1 and u = sum e^(y - m) (y - m).  The term
 // of the maximum itself is exactly 1 and is not in r, so that a small rest keeps its digits.  An empty state
@@ -713,6 +707,7 @@ template <class E, int NT>
 __global__ void __launch_bounds__(NT, NT == 256 && sizeof(typename E::storage) == 2 ? 5 : 1) top_kernel(TopArgs a) {
   using S = typename E::storage;
   constexpr int N = Dot<E>::N, WAVES = NT / 64;
+  constexpr int UNROLL = NT != 1024 ? 2 : kIsF8<E> ? 1 : 4;  // of a row's chunks (a lane of 1024 has 128 registers)
   __shared__ float side[WAVES][64];
   __shared__ float cand_v[kFineRoom];
   __shared__ int cand_g[kFineRoom], list[kCoarseRoom];
@@ -922,7 +917,7 @@ __global__ void __launch_bounds__(NT, NT == 256 && sizeof(typename E::storage) =
       const uint4* h = (const uint4*)((const S*)f.H + t * f.d);
       asm volatile("" : "+s"(h));
       double acc[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll (NT != 1024 ? 2 : kIsF8<E> ? 1 : 4)  // (a lane of 1024 has 128 registers)
+#pragma unroll UNROLL
       for (int c = lane; c < chunks; c += 64) {
         double x[N], y[N];
         uint4 raw[4];
@@ -1149,16 +1144,19 @@ static bool launch_score_stream(const ScoreArgs& a, hipStream_t s) {
 // 2048 4588 / 4440; d = 1000, V = 32003 in 5: T = 1333 806 / 760.
 template <class E> struct ScoreCfg {
   using Large = typename Cfg<E>::Logits;
+  using LargeTail = typename Cfg<E>::LogitsTail;
   using Small = typename Cfg<E>::Stream64;
   using Middle = typename Cfg<E>::Stream128;
 };
 template <> struct ScoreCfg<F8> {
   using Large = GemmF8<false>;
+  using LargeTail = GemmF8<true>;
   using Small = RingF8<64, 6>;
   using Middle = RingF8<128, 4>;
 };
 template <> struct ScoreCfg<F32> {
   using Large = Cfg<F32>::Logits;
+  using LargeTail = Cfg<F32>::LogitsTail;
   using Small = Cfg<F32>::Res128x64;
   using Middle = Cfg<F32>::Res128;
   using Least = Ring<128, 32, 4, 1, 3, F32>;
@@ -1174,7 +1172,7 @@ static bool launch_score(const ScoreArgs& a, hipStream_t s) {
     if (a.f.kind == 1) return launch_score_stream<E, typename C::Middle>(a, s);
   }
   if (a.f.d % E::KB == 0) return launch_score_g<E, typename C::Large>(a, s);
-  return launch_score_g<E, typename Cfg<E>::LogitsTail>(a, s);
+  return launch_score_g<E, typename C::LargeTail>(a, s);
 }
 
 bool run_score(int dtype, const ScoreArgs& a, hipStream_t s) {
