@@ -275,7 +275,8 @@ vp_status vp_score_forward_f8(const vp_problem* prob, const vp_score* score, con
 /* vp_ce_backward of a loss that the entropies enter, too:
  *   G[t, v] = grad_loss[t] * (p_tv - [v == targets[t]])     0 on ignored tokens
  *             - grad_entropy[t] * p_tv * (log p_tv + entropy[t])
- * NaN on out-of-range targets.  An ignored token keeps the second term.  lse, entropy: from
+ * NaN on out-of-range targets.  An ignored token keeps the second term; a term whose upstream gradient is
+ * 0 is 0, also where the entropy (or, of an ignored token, lse) is not finite.  lse, entropy: from
  * vp_score_forward on the same inputs; grad_loss, grad_entropy: device float32 [T], the upstream
  * gradients of each token's loss and entropy.  Workspace: vp_ce_workspace_size's of the
  * backward; everything else as for vp_ce_backward. */

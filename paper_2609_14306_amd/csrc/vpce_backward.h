@@ -128,9 +128,12 @@ __device__ __forceinline__ void grad_tile(const GradArgs& a, const float* entrop
     if (nl < a.N) {
       const int64_t tg = tgv[j];
       if (ENT) {
-        cexp[j] = -lsev[j] * kLog2e;
-        wg[j] = -ev[j] * sv[j];
-        wx[j] = -ev[j] * kLn2;
+        // (without an upstream gradient the entropy is not used: it may be NaN; and nor is lse without a loss)
+        if (ev[j] != 0.f || tg != a.ignore_index) cexp[j] = -lsev[j] * kLog2e;
+        if (ev[j] != 0.f) {
+          wg[j] = -ev[j] * sv[j];
+          wx[j] = -ev[j] * kLn2;
+        }
       }
       if (tg != a.ignore_index) {
         float g = gv[j];
