@@ -8,8 +8,8 @@
 //   lse = m + log(1 + r),   entropy = lse - sum p y = log(1 + r) - u / (1 + r),
 // two terms that are not negative, each to float32's relative precision: of a token of which one id holds all but
 // 1e-7 the entropy is right to 8e-6 of itself (sum e^d itself would lose 1e-7 to the 1 beside it).  Summing
-// the rest apart and exact distances take three instructions an element more: T = 4096, d = 2880, V = 201088 in
-// bfloat16 1.2%, T = 8192, d = 7168, V = 129280 in 8 bits 0.8%, narrow rows (T = 8192, d = 512, V = 50000) 6%.
+// the rest apart and exact distances take two instructions an element: T = 4096, d = 2880, V = 201088 in bfloat16
+// 1.1%, T = 8192, d = 7168, V = 129280 in 8 bits nothing, narrow rows (T = 8192, d = 512, V = 50000) 5%.
 //
 // Alternatives.  No logits are kept; the fold leaves the maximum of every four consecutive ids
 // (fine) and of the logits that a lane holds of a tile (coarse).  The K + 2 largest fine maxima,
@@ -240,11 +240,11 @@ struct RingF8 : Ring<128, BN_, 4, 2, STAGES_, F8> {
 // ---------------------------------------------------------------------------
 // A lane's state of a token: the maximum m, r = sum e^(y - m) - 1 and u = sum e^(y - m) (y - m).  The term
 // of the maximum itself is exactly 1 and is not in r, so that a small rest keeps its digits.  An empty state
-// has m = kNoLogit and r = -1, the sum 0.
+// has m = kNoLogit, whose e^(y - m) is 0 beside any logit, and r = -1, the sum 0, where it leaves the workgroup.
 struct Fold {
   float m, r, u;
 };
-constexpr float kLeast = -1e4f;  // e^kLeast is 0: the distance that farther logits are held to
+constexpr float kLeast = -1e4f;  // e^kLeast is 0: the distance that farther maxima are held to
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 // The state with the maximum `m` in place of its own, which is no larger: its whole sum is part of r then.
 __device__ __forceinline__ Fold rescaled(Fold f, float m) {
@@ -268,7 +268,7 @@ constexpr int kFineTokens = G::SKIPS ? 32 : 1;
 // TOP, leaves its maxima: fine, the bm / 4 ones of this tile and the lane's token, and coarse
 // (both null for a token that does not exist).  Rows from `lim` on are minus infinity.
 template <int MB, int NB, bool TOP, int TOK>
-__device__ __forceinline__ void fold_score(const f32x16_t (&acc)[MB][NB], int j, bool full, int lim, Fold& f,
+__device__ __forceinline__ void fold_score(f32x16_t (&acc)[MB][NB], int j, bool full, int lim, Fold& f,
                                            int lane, float* fine, float* coarse) {
   float g[MB][4], top = -INFINITY;
 #pragma unroll
@@ -312,17 +312,32 @@ __device__ __forceinline__ void fold_score(const f32x16_t (&acc)[MB][NB], int j,
   }
   const float m = fmaxf(f.m, top);
   // s - rest are the terms of 1 (the maximum, and what equals it): rest leaves them out, and keeps its digits.
-  float s = 0.f, rest = 0.f, u = 0.f;
+  float s, rest, u;
+  for (bool low = !full;; low = true) {
+    // e^d d of a logit of minus infinity is 0, not 0 times infinity.  Where there is one, as in the dead rows of a
+    // shard's last tile, they are raised to a distance whose e^d is 0, too (a maximum with every d costs 1%).
+    if (low) {
+      const float least = fmaxf(m - fmaxf(2000.f, __builtin_fabsf(m)), kNoLogit);
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    if (i > 0) __builtin_amdgcn_sched_barrier(0);  // (16 exponents at a time: more of them are spilled)
+      for (int i = 0; i < MB; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float d = acc[i][j][r] - m, e = exp_of(d);
-      s += e;
-      rest += __builtin_amdgcn_fractf(e);
-      u = __builtin_fmaf(e, fmaxf(d, kLeast), u);
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = acc[i][j][r] < least ? least : acc[i][j][r];
     }
+    s = rest = u = 0.f;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      if (i > 0) __builtin_amdgcn_sched_barrier(0);  // (16 exponents at a time: more of them are spilled)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float d = acc[i][j][r] - m, e = exp_of(d);
+        s += e;
+        rest += __builtin_amdgcn_fractf(e);
+        u = __builtin_fmaf(e, d, u);
+      }
+      // (the sums are made here: the compiler would hold all exponentials for them until the loop's end)
+      asm volatile("" : "+v"(s), "+v"(rest), "+v"(u));
+    }
+    if (low || !__any(u != u)) break;
   }
   const bool rises = m > f.m;  // one of the terms of 1 is the new maximum
   if (rises) f = rescaled(f, m);
@@ -388,8 +403,9 @@ __device__ __forceinline__ void write_folds(const ScoreArgs& a, Fold (&f)[G::NB]
       }
       const int64_t n = n0 + c;
       if (n < a.f.T) {
-        a.f.m_part[(int64_t)split * a.f.T + n] = f[j].m == kNoLogit ? -INFINITY : f[j].m;
-        a.f.s_part[(int64_t)split * a.f.T + n] = f[j].r;
+        const bool none = f[j].m == kNoLogit;
+        a.f.m_part[(int64_t)split * a.f.T + n] = none ? -INFINITY : f[j].m;
+        a.f.s_part[(int64_t)split * a.f.T + n] = none && f[j].r >= 0.f ? -1.f : f[j].r;  // (or NaN)
         a.u_part[(int64_t)split * a.f.T + n] = f[j].u;
       }
     }
