@@ -565,8 +565,8 @@ def backward(H, W_shards: List, targets, lse, grad_loss, ignore_index: int = -10
     """(dH [T, d], [dW_p [V_p, d]]) float32, recomputing the logits from the saved lse.
 
     With `grad_entropy` [T], the upstream gradient of each token's entropy, and `entropy` [T] (both
-    from ``score``, which gives the same loss and lse as ``forward``), the gradients of a loss with an
-    entropy term.
+    from ``score``, whose loss and lse are those of ``forward`` but for roundings), the gradients of a loss
+    with an entropy term.
 
     With `norm` (as given to `forward`): (dH, [dW_p], dgamma, dbeta) with the gradient of the
     norm's input as dH, written over that of its result; the norm is recomputed.  dbeta is None

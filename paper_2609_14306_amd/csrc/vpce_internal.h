@@ -74,7 +74,9 @@ struct ScoreArgs {
   int32_t nb;
 };
 
-constexpr int kF8MaxBlocks = 112;  // 128-column blocks that a token's scales may be of
+// 128-column blocks that a token's scales may be of: the ring of the 256 x 256 tile takes 128 KiB of LDS, the scales of
+// its 256 tokens 28 KiB with 112 blocks, and what is left holds those of its vocabulary tiles.
+constexpr int kF8MaxBlocks = 112;
 constexpr int kF8MaxD = 128 * kF8MaxBlocks;
 
 struct ScoreCombArgs {

@@ -27,15 +27,15 @@
 // of the logits' spread.  Over many ids that averages out; where a few hold the probability it does not
 // (logits of spread 4: entropies 1e-5 off).  So the ids with a probability of 2^-7 and more have their
 // exact logits put into lse and entropy behind the fold (top_kernel, kHeavy): 1e-7 to 8e-7 then.  That
-// takes the maxima also without alternatives (T = 8192, d = 7168, V = 129280 6% of the time).  Widened to
+// takes the maxima also without alternatives (T = 8192, d = 7168, V = 129280 6% of the time, half of it that kernel's).  Widened to
 // bfloat16, where the products are exact, few tokens took 164 us instead of 132 (T = 1 to 64, V = 151936,
 // d = 4096), with one wavefront a SIMD 137 (T to 32) and 183, and large tiles would run at half the rate.
 //
 // What bounds it (kernels alone).  Many tokens: the matrix rate at the clock that the chip's power
-// leaves: T = 4096, d = 2880, V = 201088 in bfloat16 3.69 ms (1284 TFLOP/s, as vp_ce_forward; 3.88 and 0.20
-// for the ranking with 8 alternatives), T = 8192, d = 7168, V = 129280 in 8 bits 5.71 ms (2660; 5.46 without maxima) and 0.19, T = 1000, d =
-// 7168, V = 32000 in float32 3.36 ms (137).  Few tokens: reading W: T = 1, d = 4096, V = 151936 in bfloat16
-// 218 us (5.7 TB/s) and 30 for 20 alternatives, T = 40 in 8 bits 121 us (5.2 TB/s) and 18 for 5.
+// leaves: T = 4096, d = 2880, V = 201088 in bfloat16 3.65 ms (1301 TFLOP/s, as vp_ce_forward; 3.87 and 0.23 for the
+// ranking with 8 alternatives), T = 8192, d = 7168, V = 129280 in 8 bits 5.58 ms (2720) and 0.19, T = 1000, d = 7168,
+// V = 32000 in float32 3.36 ms (136).  Few tokens: reading W: T = 1, d = 4096, V = 151936 in bfloat16 226 us (208 at
+// best, 6.0 TB/s) and 31 for 20 alternatives, T = 40 in 8 bits 131 us (117 at best, 5.3 TB/s) and 21 for 5.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
