@@ -27,9 +27,9 @@
 // of the logits' spread.  Over many ids that averages out; where a few hold the probability it does not
 // (logits of spread 4: entropies 1e-5 off).  So the ids with a probability of 2^-7 and more have their
 // exact logits put into lse and entropy behind the fold (top_kernel, kHeavy): 1e-7 to 8e-7 then.  That
-// takes the maxima also without alternatives (T = 8192, d = 7168, V = 129280 6% of the time, half of it that kernel's).  Widened to
-// bfloat16, where the products are exact, few tokens took 164 us instead of 132 (T = 1 to 64, V = 151936,
-// d = 4096), with one wavefront a SIMD 137 (T to 32) and 183, and large tiles would run at half the rate.
+// takes the maxima also without alternatives (T = 8192, d = 7168, V = 129280 6% of the time, half of it that
+// kernel's).  Widened to bfloat16, where the products are exact, few tokens took 164 us instead of 132 (T = 1 to 64,
+// V = 151936, d = 4096), with one wavefront a SIMD 137 (T to 32) and 183, and large tiles would run at half the rate.
 //
 // What bounds it (kernels alone).  Many tokens: the matrix rate at the clock that the chip's power
 // leaves: T = 4096, d = 2880, V = 201088 in bfloat16 3.65 ms (1301 TFLOP/s, as vp_ce_forward; 3.87 and 0.23 for the
